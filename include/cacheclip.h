@@ -258,10 +258,127 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
                             int64_t stride_token, int64_t stride_head, int32_t n_tail,
                             const cc_kv_layer* dst);
 
+/* ---- the paged cache of the answer phase ----
+ *
+ * What follows the recomputed prompt: sequences that grow by single tokens or by chunks (a follow-up
+ * question), answers that fork from one context, and what is freed behind them.  Keys and values live in pages of
+ * page_size tokens that sequences hold by reference.  A cache of cc_recompute_layer becomes pages without a copy
+ * when its slots are a multiple of page_size: stride_page = page_size * stride_token, page i = slots i*page_size ...
+ *
+ * All of it is device memory of the caller, and every change is made on the device in stream order, so that a decode
+ * loop needs no host round trip and can be captured.
+ *   refs    [n_pages]             holders of a page; 0 = free
+ *   table   [n_seqs, max_pages]   row stride stride_table; entry c of sequence s: the page of its tokens
+ *           c*page_size ..; a sequence of len tokens holds its first ceil(len / page_size) entries, the others
+ *           are not read (cc_free_pages leaves -1 there)
+ *   len     [n_seqs]              tokens; 0 = the row is free
+ *   status  [1]                   result of the last of the four calls below: 0 or a cc_status
+ *   work    cc_page_work_bytes(n_pages, n_seqs) bytes, 256-byte aligned: scratch, its contents mean nothing
+ *           between calls.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
+ *           at once), whatever context they come from.
+ * page_size is a power of two, 16 to 1024; n_seqs <= 65536, n_pages * page_size < 2^31. */
+typedef struct cc_page_pool {
+    int32_t* refs;
+    int32_t* table;
+    int32_t* len;
+    int32_t* status;
+    void* work;
+    int64_t work_bytes;
+    int64_t stride_table;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_seqs;
+    int32_t max_pages;
+} cc_page_pool;
+int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs);
+
+/* One layer's pages, dev bf16: element (page, token, head, c) of K and V is at
+ * page*stride_page + token*stride_token + head*stride_head + c (elements; strides multiples of 8, c contiguous,
+ * tokens or heads outermost in a page).  Slots behind a sequence's last token may hold anything; the others must be
+ * finite, as everywhere in this library.  A page outside [0, n_pages) reads as zeros and is never written, so that
+ * pages which slid out of every window may be given back. */
+typedef struct cc_paged_kv {
+    void* K;
+    void* V;
+    int64_t stride_page;
+    int64_t stride_token;
+    int64_t stride_head;
+} cc_paged_kv;
+
+/* New tokens of a batch: rows start[b] .. start[b+1]-1 of q, k, v and o are the last tokens of sequence
+ * seq[b] (b itself where seq is NULL); row r sits at position len - (start[b+1] - start[b]) + r - start[b], its length
+ * already counts it (cc_grow_pages).  A sequence without rows is allowed.  Rows that belong to no sequence
+ * (in front of start[0], behind start[n]) are neither read nor written. */
+typedef struct cc_new_rows {
+    const int32_t* start;   /* dev [n + 1], ascending, within [0, rows] */
+    const int32_t* seq;     /* dev [n], each in [0, n_seqs), or NULL */
+    int32_t n;              /* sequences, 0 to 2048 */
+    int32_t rows;           /* rows of the buffers */
+    int32_t max_new;        /* most rows of any sequence, as a bound: it only decides launch shapes */
+} cc_new_rows;
+
+/* Makes room for n_new[i] >= 0 more tokens of sequence seq[i] (dev int32 [n], distinct): its length grows by them and
+ * it takes the pages it lacks, the lowest free ones, in the order of the list.  Where its last page is shared and not full
+ * it first takes a page for a copy of that page's tokens, made in every layer (kv: host array [n_layers], read
+ * during the call only, all with the same strides), so that it can be written to.  All or nothing: with too few free
+ * pages status is CC_ERR_WORKSPACE, with more than max_pages for a sequence CC_ERR_SHAPE, with a bad or
+ * repeated index CC_ERR_IDX, and nothing has changed.
+ * status_host (host, or NULL): if given the call waits for the status and also returns it. */
+cc_status cc_grow_pages(cc_ctx* ctx, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers,
+                        const int32_t* seq, const int32_t* n_new, int32_t n, int32_t* status_host);
+/* Sequence dst[i] (dev int32 [n], distinct, each of length 0) becomes a second holder of all that src[i] holds at the
+ * call; src may repeat.  No keys or values are copied.  CC_ERR_IDX as above. */
+cc_status cc_fork_pages(cc_ctx* ctx, const cc_page_pool* pool, const int32_t* src, const int32_t* dst, int32_t n,
+                        int32_t* status_host);
+/* Sequences seq[i] (dev int32 [n], distinct) give back what they hold; their lengths become 0. */
+cc_status cc_free_pages(cc_ctx* ctx, const cc_page_pool* pool, const int32_t* seq, int32_t n, int32_t* status_host);
+/* Moves the pages in use to the front: with L pages in use, the i-th of them that lies at L or behind goes to
+ * the i-th free page in front of L, in every layer; refs and every sequence's entries follow. */
+cc_status cc_compact_pages(cc_ctx* ctx, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers,
+                           int32_t* status_host);
+
+/* Rotary rule: the first `rot` elements of a head turn in pairs (j, j + rot/2), or (2j, 2j + 1) where interleaved, by
+ * the angle position * w_j; the others pass through.  w_j = base^(-2j/rot), and for contexts longer than the model was
+ * trained on (factor >= 1, orig_len tokens, low < high in turns within orig_len):
+ *   CC_ROPE_LINEAR  w_j / factor
+ *   CC_ROPE_TURNS   w_j ((1-g)/factor + g), g = clamp((orig_len w_j / 2pi - low) / (high - low), 0, 1)
+ *   CC_ROPE_INDEX   the same with g = 1 - clamp((j - lo) / max(hi - lo, 0.001), 0, 1), where lo and hi are the pair indexes
+ *                   j(t) = rot ln(orig_len / (2pi t)) / (2 ln base) at t = high, rounded down and at least 0, and at
+ *                   t = low, rounded up and at most rot - 1
+ * The turned pair is multiplied by mscale (the attention temperature of a scaled context; 1 where there is none). */
+enum { CC_ROPE_PLAIN = 0, CC_ROPE_LINEAR = 1, CC_ROPE_TURNS = 2, CC_ROPE_INDEX = 3 };
+typedef struct cc_rope {
+    double base;            /* > 1 */
+    int32_t rot;            /* even, 2 .. d_h */
+    int32_t interleaved;
+    int32_t scaling;
+    int32_t orig_len;
+    double factor, low, high, mscale;
+} cc_rope;
+
+/* Rotary positions of new rows and their keys and values into the pages.  q dev bf16 [rows, H_q*d_h], k and v
+ * [rows, H_kv*d_h], row strides in elements (the three parts of one QKV product, for instance); q_out dev bf16
+ * [rows, H_q*d_h], contiguous: the turned queries (it may be q itself where q's rows are contiguous).
+ * pos dev int32 [rows], or NULL: the position each row turns by where it is not the row's place in the sequence.
+ * A sequence must not be listed twice, and a page that another sequence also holds is written all the same:
+ * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths and the written pages first;
+ * without it, rows in front of their sequence's first token are skipped. */
+cc_status cc_step_rope_append(cc_ctx* ctx, const void* q, int64_t stride_q, const void* k, int64_t stride_k,
+                              const void* v, int64_t stride_v, const cc_new_rows* rows, const int32_t* pos,
+                              const cc_page_pool* pool, const cc_paged_kv* kv, const cc_rope* rope, void* q_out,
+                              int32_t flags);
+/* Attention of new rows over the paged cache, grouped-query and causal: the row at position p sees key j <= p if window
+ * is 0, j > p - window (the newest `window` keys, its own among them) or j < sinks.  q (turned) and o dev bf16
+ * [rows, H_q*d_h].  A row that sees nothing (in front of its sequence's first token) gets zeros.
+ * flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths and the pages that some row sees first. */
+cc_status cc_step_paged_attention(cc_ctx* ctx, const void* q, const cc_new_rows* rows, const cc_page_pool* pool,
+                                  const cc_paged_kv* kv, int32_t window, int32_t sinks, void* o, int32_t flags);
+
 /* ---- timing of the library's own kernels on its stream ---- */
 enum {
     CC_K_COLSUM = 0, CC_K_SELECT, CC_K_GATHER_NORM, CC_K_QKV, CC_K_ATTN, CC_K_OPROJ,
     CC_K_POST_NORM, CC_K_GATE_UP, CC_K_DOWN, CC_K_ASSEMBLE, CC_K_COPY, CC_K_BLOCK_SCORES,
+    CC_K_ROPE_APPEND, CC_K_PAGED_ATTN, CC_K_PAGES, CC_K_PAGE_COPY,
     CC_K_COUNT
 };
 /* While enabled, every kernel launch is bracketed by HIP events on the stream. */

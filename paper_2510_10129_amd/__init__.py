@@ -7,6 +7,6 @@ there is no CPU or PyTorch fallback, and importing this package fails loudly
 if the library has not been built.
 """
 from ._lib import (  # noqa: F401
-    CacheClipError, Context, LayerWeights, KVLayer, ModelDesc, lib_path, load_library,
-    K_NAMES, select_noalloc,
+    CacheClipError, Context, LayerWeights, KVLayer, ModelDesc, NewRows, PagedKV, PagePool, Rope, lib_path,
+    load_library, K_NAMES, select_noalloc,
 )

@@ -19,7 +19,8 @@ CC_OK = 0
 CC_ERR_NULL, CC_ERR_SHAPE, CC_ERR_IDX, CC_ERR_WORKSPACE, CC_ERR_HIP = -1, -2, -3, -4, -5
 FLAG_NO_GROUPING, FLAG_CHECK_IDX = 1, 2
 K_NAMES = ("colsum", "select", "gather_norm", "qkv", "attn", "oproj", "post_norm", "gate_up", "down",
-           "assemble", "copy", "block_scores")
+           "assemble", "copy", "block_scores", "rope_append", "paged_attn", "pages", "page_copy")
+ROPE_SCALINGS = ("plain", "linear", "turns", "index")
 
 EXPORTS = (
     "cc_create", "cc_destroy", "cc_set_stream", "cc_last_error", "cc_select",
@@ -27,6 +28,8 @@ EXPORTS = (
     "cc_step_qkv_rope_scatter", "cc_step_sparse_attention", "cc_step_oproj_residual",
     "cc_step_mlp", "cc_profile_enable", "cc_profile_read", "cc_calib_copy", "cc_assemble_cache",
     "cc_step_block_scores", "cc_select_blocks", "cc_debug_set_launch", "cc_select_noalloc",
+    "cc_page_work_bytes", "cc_grow_pages", "cc_fork_pages", "cc_free_pages", "cc_compact_pages",
+    "cc_step_rope_append", "cc_step_paged_attention",
 )
 
 
@@ -64,6 +67,27 @@ class _Weights(C.Structure):
 class LaunchOverride(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("gemm_tile", "gemm_staged", "gemm_mfma32", "gemm_gm",
                                          "gemm_splitk", "attn_splits")]
+
+
+class _Pool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("refs", "table", "len", "status", "work")] + [
+        ("work_bytes", C.c_int64), ("stride_table", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+        ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class _PagedKV(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("stride_page", C.c_int64), ("stride_token", C.c_int64),
+                ("stride_head", C.c_int64)]
+
+
+class _NewRows(C.Structure):
+    _fields_ = [("start", C.c_void_p), ("seq", C.c_void_p), ("n", C.c_int32), ("rows", C.c_int32), ("max_new", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("base", C.c_double), ("rot", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32),
+                ("orig_len", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("mscale", C.c_double)]
 
 
 def lib_path() -> str:
@@ -113,9 +137,19 @@ def load_library() -> C.CDLL:
     lib.cc_debug_set_launch.argtypes = [vp, C.POINTER(LaunchOverride)]
     lib.cc_profile_enable.argtypes = [vp, i32]
     lib.cc_profile_read.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(i32)]
+    lib.cc_page_work_bytes.argtypes = [i32, i32]
+    lib.cc_grow_pages.argtypes = [vp, C.POINTER(_Pool), C.POINTER(_PagedKV), i32, vp, vp, i32, C.POINTER(i32)]
+    lib.cc_fork_pages.argtypes = [vp, C.POINTER(_Pool), vp, vp, i32, C.POINTER(i32)]
+    lib.cc_free_pages.argtypes = [vp, C.POINTER(_Pool), vp, i32, C.POINTER(i32)]
+    lib.cc_compact_pages.argtypes = [vp, C.POINTER(_Pool), C.POINTER(_PagedKV), i32, C.POINTER(i32)]
+    lib.cc_step_rope_append.argtypes = [vp, vp, i64, vp, i64, vp, i64, C.POINTER(_NewRows), vp, C.POINTER(_Pool),
+                                        C.POINTER(_PagedKV), C.POINTER(_Rope), vp, i32]
+    lib.cc_step_paged_attention.argtypes = [vp, vp, C.POINTER(_NewRows), C.POINTER(_Pool), C.POINTER(_PagedKV), i32, i32, vp,
+                                            i32]
     for name in EXPORTS:
         if name != "cc_last_error":
             getattr(lib, name).restype = i32
+    lib.cc_page_work_bytes.restype = i64
     _lib = lib
     return lib
 
@@ -148,6 +182,119 @@ class KVLayer:
         K, V = self.K, self.V
         assert K.shape == V.shape and K.stride() == V.stride() and K.stride(2) == 1
         return _KV(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.shape[0])
+
+
+def _i32(t, what: str, dims: int = 1):
+    """A device list as the library reads it: int32, unit stride."""
+    if t.dtype != _torch().int32 or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what} must be an int32 tensor of {dims} dimension(s) with unit stride")
+    return t
+
+
+def _bf16(t, what: str):
+    if t.dtype != _torch().bfloat16:
+        raise ValueError(f"{what} must be a bfloat16 tensor")
+    return t
+
+
+def _torch():
+    import torch
+    return torch
+
+
+@dataclass
+class PagePool:
+    """Pages that sequences hold by reference: refs [n_pages], table [n_seqs, max_pages], len [n_seqs] int32 on
+    the device, page_size tokens a page.  status and work are allocated where they are not given.  `PagePool.empty`
+    makes one with every page free."""
+    refs: "object"
+    table: "object"
+    len: "object"
+    page_size: int
+    status: "object" = None
+    work: "object" = None
+
+    def __post_init__(self):
+        torch = _torch()
+        _i32(self.refs, "refs"), _i32(self.table, "table", 2), _i32(self.len, "len")
+        if self.table.shape[0] != self.len.shape[0]:
+            raise ValueError("table and len must have a row for each sequence")
+        if self.status is None:
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.refs.device)
+        if _i32(self.status, "status").numel() < 1:
+            raise ValueError("status must hold one value")
+        if self.work is None:
+            size = load_library().cc_page_work_bytes(self.refs.numel(), self.len.numel())
+            self.work = torch.empty(size, dtype=torch.uint8, device=self.refs.device)
+        if not self.work.is_contiguous():
+            raise ValueError("work must be contiguous")
+        for t in (self.table, self.len, self.status, self.work):
+            if t.device != self.refs.device:
+                raise ValueError("a pool's tensors must lie on one device")
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_seqs: int, max_pages: int, device="cuda"):
+        torch = _torch()
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(n_pages, **i32), torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32), page_size)
+
+    def c_struct(self) -> _Pool:
+        return _Pool(self.refs.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.status.data_ptr(),
+                     self.work.data_ptr(), self.work.numel() * self.work.element_size(), self.table.stride(0),
+                     self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1])
+
+
+@dataclass
+class PagedKV:
+    """One layer's pages: K, V torch bf16 tensors [n_pages, page_size, H_kv, d_h] (last dim contiguous; a view of
+    [n_pages, H_kv, page_size, d_h] will do)."""
+    K: "object"
+    V: "object"
+
+    def c_struct(self, pool: PagePool, model) -> _PagedKV:
+        K, V = _bf16(self.K, "K"), _bf16(self.V, "V")
+        shape = (pool.refs.numel(), pool.page_size, model.H_kv, model.d_h)
+        if K.shape != shape or V.shape != shape or K.stride() != V.stride() or K.stride(3) != 1:
+            raise ValueError(f"K and V must be {shape} with equal strides, the last of them 1")
+        if K.device != pool.refs.device or V.device != pool.refs.device:
+            raise ValueError("pages must lie on the pool's device")
+        return _PagedKV(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2))
+
+
+@dataclass
+class NewRows:
+    """New tokens of a batch: start int32 [n + 1] on the device, seq int32 [n] or None (sequence b is row b of the table),
+    rows of the buffers, and a bound on the rows of one sequence."""
+    start: "object"
+    seq: "object"
+    rows: int
+    max_new: int
+
+    def c_struct(self) -> _NewRows:
+        n = _i32(self.start, "start").numel() - 1
+        if n < 0 or (self.seq is not None and _i32(self.seq, "seq").numel() != n):
+            raise ValueError("start must have one entry more than seq")
+        return _NewRows(self.start.data_ptr(), _ptr(self.seq), n, self.rows, self.max_new)
+
+
+@dataclass
+class Rope:
+    """A rotary rule (cc_rope): scaling is "plain", "linear", "turns" or "index"."""
+    base: float
+    rot: int
+    interleaved: bool = False
+    scaling: str = "plain"
+    factor: float = 1.0
+    orig_len: int = 0
+    low: float = 1.0
+    high: float = 4.0
+    mscale: float = 1.0
+
+    def c_struct(self) -> _Rope:
+        if self.scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
+        return _Rope(self.base, self.rot, int(self.interleaved), ROPE_SCALINGS.index(self.scaling), self.orig_len, self.factor,
+                     self.low, self.high, self.mscale)
 
 
 @dataclass
@@ -317,6 +464,63 @@ class Context:
         arr = (_Chunk * n).from_buffer(array("Q", flat))
         kvs = dst.c_struct()
         self._check(self._lib.cc_assemble_cache(self._h, arr, n, P, st[0], st[1], n_tail, C.byref(kvs)))
+
+    # ---- the paged cache of the answer phase ----
+    def _layers(self, pool: PagePool, kvs: Sequence[PagedKV]):
+        return (_PagedKV * len(kvs))(*[kv.c_struct(pool, self.desc) for kv in kvs]), len(kvs)
+
+    def _pages(self, call, pool: PagePool, sync: bool, *args):
+        p, host = pool.c_struct(), C.c_int32(0)
+        self._check(call(self._h, C.byref(p), *args, C.byref(host) if sync else None))
+
+    @staticmethod
+    def _seqs(a, b):
+        if _i32(a, "sequences").numel() != _i32(b, "their second list").numel():
+            raise ValueError("the two lists must have the same length")
+        return a.data_ptr(), b.data_ptr(), a.numel()
+
+    def grow_pages(self, pool: PagePool, kvs: Sequence[PagedKV], seq, n_new, sync: bool = True):
+        """Room for n_new[i] more tokens of sequence seq[i].  sync: waits for the device's status and raises on an error;
+        without it pool.status says how the call ended (so for the three calls below)."""
+        arr, n_layers = self._layers(pool, kvs)
+        self._pages(self._lib.cc_grow_pages, pool, sync, arr, n_layers, *self._seqs(seq, n_new))
+
+    def fork_pages(self, pool: PagePool, src, dst, sync: bool = True):
+        self._pages(self._lib.cc_fork_pages, pool, sync, *self._seqs(src, dst))
+
+    def free_pages(self, pool: PagePool, seq, sync: bool = True):
+        self._pages(self._lib.cc_free_pages, pool, sync, _i32(seq, "seq").data_ptr(), seq.numel())
+
+    def compact_pages(self, pool: PagePool, kvs: Sequence[PagedKV], sync: bool = True):
+        self._pages(self._lib.cc_compact_pages, pool, sync, *self._layers(pool, kvs))
+
+    def _row_buffer(self, t, what: str, rows: int, width: int):
+        if _bf16(t, what).shape != (rows, width) or t.stride(1) != 1:
+            raise ValueError(f"{what} must be [{rows}, {width}] with unit column stride")
+        return t.stride(0) if rows > 1 else width
+
+    def step_rope_append(self, q, k, v, new: NewRows, pool: PagePool, kv: PagedKV, rope: Rope, q_out, pos=None, flags: int = 0):
+        """q [rows, H_q*d_h], k, v [rows, H_kv*d_h] cuda bf16 (column slices of one product will do) -> q_out, pages of kv."""
+        m = self.desc
+        nq, nk = m.H_q * m.d_h, m.H_kv * m.d_h
+        st = [self._row_buffer(t, w, new.rows, n) for t, w, n in ((q, "q", nq), (k, "k", nk), (v, "v", nk))]
+        if self._row_buffer(q_out, "q_out", new.rows, nq) != nq:
+            raise ValueError("q_out must be contiguous")
+        if pos is not None and _i32(pos, "pos").numel() < new.rows:
+            raise ValueError("pos must have an entry for each row")
+        p, kvs, r, rule = pool.c_struct(), kv.c_struct(pool, m), new.c_struct(), rope.c_struct()
+        self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st[0], k.data_ptr(), st[1], v.data_ptr(), st[2], C.byref(r),
+                                                  _ptr(pos), C.byref(p), C.byref(kvs), C.byref(rule), q_out.data_ptr(), flags))
+
+    def step_paged_attention(self, q, new: NewRows, pool: PagePool, kv: PagedKV, o, window: int = 0, sinks: int = 0, flags: int = 0):
+        """q, o cuda bf16 [rows, H_q*d_h], contiguous."""
+        m = self.desc
+        for t, what in ((q, "q"), (o, "o")):
+            if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
+                raise ValueError(f"{what} must be contiguous")
+        p, kvs, r = pool.c_struct(), kv.c_struct(pool, m), new.c_struct()
+        self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,
+                                                      o.data_ptr(), flags))
 
     # ---- measurement support ----
     def calib_copy(self, dst, src):

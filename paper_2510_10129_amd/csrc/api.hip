@@ -7,6 +7,7 @@
 
 #include "cc_internal.h"
 #include "launch_plan.h"
+#include "paged.h"
 
 // Scratch of cc_select_noalloc: the importance scores between its two kernels live here
 // instead of in a context's workspace.  One copy per GPU, held until the process ends.  In host
@@ -59,6 +60,17 @@ cc_status fail(cc_ctx* c, cc_status code, const std::string& msg) {
             return fail((c), CC_ERR_HIP, std::string(#call) + ": " + hipGetErrorString(e_)); \
     } while (0)
 
+// Makes the context's device current for a call, whatever device the caller has current.
+struct device_scope {
+    int before = -1, dev;
+    explicit device_scope(int d) : dev(d) {
+        if (hipGetDevice(&before) == hipSuccess && before != dev) (void)hipSetDevice(dev);
+    }
+    ~device_scope() {
+        if (before >= 0 && before != dev) (void)hipSetDevice(before);
+    }
+};
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 cc_status check_model(const cc_model_desc& m, std::string* why) {
@@ -103,6 +115,29 @@ cc_status check_idx_sync(cc_ctx* c, const int32_t* idx, int M, int hi, int stric
     if (c->pinned[0] != 0)
         return fail(c, CC_ERR_IDX, std::string(what) + (strict ? " must be strictly ascending and in range"
                                                                 : " must be in range"));
+    return CC_OK;
+}
+
+// Whether the rows of a batch fit their pool; synchronises the stream.
+cc_status check_rows_sync(cc_ctx* c, const cc_new_rows& r, const cc_page_pool& p, int window, int sinks, int append) {
+    CC_HIP(c, hipMemsetAsync(c->flag, 0, sizeof(int32_t), c->stream));
+    cc_launch_check_rows(r, p, window, sinks, append, c->flag, c->stream);
+    CC_HIP(c, hipMemcpyAsync(c->pinned, c->flag, sizeof(int32_t), hipMemcpyDeviceToHost, c->stream));
+    CC_HIP(c, hipStreamSynchronize(c->stream));
+    if (c->pinned[0] != 0)
+        return fail(c, CC_ERR_IDX, "start must ascend within rows, seq be in range, a sequence be as long as its new rows and its pages be in range");
+    return CC_OK;
+}
+
+// What cc_grow_pages and its like return: the launch's own error, then, if asked for, the device's status.
+cc_status pages_result(cc_ctx* c, int32_t* status_host) {
+    CC_HIP(c, hipGetLastError());
+    if (!status_host) return CC_OK;
+    CC_HIP(c, hipStreamSynchronize(c->stream));
+    const cc_status st = *status_host = c->pinned[2];
+    if (st == CC_ERR_IDX) return fail(c, st, "a sequence index is out of range or repeated, a new sequence is not empty, or a count is negative");
+    if (st == CC_ERR_SHAPE) return fail(c, st, "a sequence would need more than max_pages pages");
+    if (st == CC_ERR_WORKSPACE) return fail(c, st, "too few free pages");
     return CC_OK;
 }
 
@@ -196,7 +231,7 @@ cc_status cc_create(cc_ctx** out, const cc_model_desc* desc, void* hip_stream) {
     }
     alloc((void**)&c->n_sel, 4);
     alloc((void**)&c->flag, 4);
-    if (e == hipSuccess) e = hipHostMalloc((void**)&c->pinned, 2 * sizeof(int32_t), hipHostMallocDefault);
+    if (e == hipSuccess) e = hipHostMalloc((void**)&c->pinned, 4 * sizeof(int32_t), hipHostMallocDefault);
     if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->pinned_dev, c->pinned, 0);
     if (e != hipSuccess) {
         std::string msg = std::string("workspace allocation: ") + hipGetErrorString(e);
@@ -568,6 +603,127 @@ cc_status cc_assemble_cache(cc_ctx* c, const cc_chunk_kv* chunks, int32_t n_chun
             a.n_blocks = nb;
             cc_launch_assemble(a, c->rope, c->m, stride_token, stride_head, *dst, c->stream);
         }
+    }
+    CC_HIP(c, hipGetLastError());
+    return CC_OK;
+}
+
+#define CC_REFUSE(c, call)                                                          \
+    do {                                                                            \
+        const cc_refusal r_ = (call);                                               \
+        if (r_.code != CC_OK) return fail((c), r_.code, r_.why);                    \
+    } while (0)
+
+int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs) {
+    if (n_pages < 1 || n_seqs < 1) return 0;
+    return cc_page_work_size(n_pages, n_seqs);
+}
+
+cc_status cc_grow_pages(cc_ctx* c, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers, const int32_t* seq,
+                        const int32_t* n_new, int32_t n, int32_t* status_host) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_layers(kv, n_layers, pool->page_size, c->m.H_kv, c->m.d_h));
+    CC_REFUSE(c, cc_check_list(n, pool->n_seqs, seq, n_new));
+    device_scope dev(c->device);
+    {
+        cc_prof_scope ps(c, CC_K_PAGES);
+        cc_launch_grow(*pool, seq, n_new, n, status_host ? c->pinned_dev + 2 : nullptr, c->stream);
+    }
+    if (n > 0) {
+        cc_prof_scope ps(c, CC_K_PAGE_COPY);
+        cc_launch_page_copies(*pool, kv, n_layers, n, c->m.H_kv, c->m.d_h, c->stream);
+    }
+    return pages_result(c, status_host);
+}
+
+cc_status cc_fork_pages(cc_ctx* c, const cc_page_pool* pool, const int32_t* src, const int32_t* dst, int32_t n,
+                        int32_t* status_host) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_list(n, pool->n_seqs, src, dst));
+    device_scope dev(c->device);
+    {
+        cc_prof_scope ps(c, CC_K_PAGES);
+        cc_launch_fork(*pool, src, dst, n, status_host ? c->pinned_dev + 2 : nullptr, c->stream);
+    }
+    return pages_result(c, status_host);
+}
+
+cc_status cc_free_pages(cc_ctx* c, const cc_page_pool* pool, const int32_t* seq, int32_t n, int32_t* status_host) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_list(n, pool->n_seqs, seq, seq));
+    device_scope dev(c->device);
+    {
+        cc_prof_scope ps(c, CC_K_PAGES);
+        cc_launch_free(*pool, seq, n, status_host ? c->pinned_dev + 2 : nullptr, c->stream);
+    }
+    return pages_result(c, status_host);
+}
+
+cc_status cc_compact_pages(cc_ctx* c, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers, int32_t* status_host) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_layers(kv, n_layers, pool->page_size, c->m.H_kv, c->m.d_h));
+    device_scope dev(c->device);
+    {
+        cc_prof_scope ps(c, CC_K_PAGES);
+        cc_launch_compact(*pool, status_host ? c->pinned_dev + 2 : nullptr, c->stream);
+    }
+    {
+        cc_prof_scope ps(c, CC_K_PAGE_COPY);
+        cc_launch_page_copies(*pool, kv, n_layers, (pool->n_pages + 1) / 2, c->m.H_kv, c->m.d_h, c->stream);
+    }
+    return pages_result(c, status_host);
+}
+
+cc_status cc_step_rope_append(cc_ctx* c, const void* q, int64_t stride_q, const void* k, int64_t stride_k, const void* v,
+                              int64_t stride_v, const cc_new_rows* rows, const int32_t* pos, const cc_page_pool* pool,
+                              const cc_paged_kv* kv, const cc_rope* rope, void* q_out, int32_t flags) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_paged_kv(kv, pool->page_size, c->m.H_kv, c->m.d_h));
+    CC_REFUSE(c, cc_check_new_rows(rows, pool->n_seqs, c->m.H_q / c->m.H_kv));
+    CC_REFUSE(c, cc_check_rope(rope, c->m.d_h));
+    if (rows->rows > 0 && (!q || !k || !v || !q_out)) return fail(c, CC_ERR_NULL, "q, k, v and q_out must not be NULL");
+    const int64_t nq = (int64_t)c->m.H_q * c->m.d_h, nk = (int64_t)c->m.H_kv * c->m.d_h;
+    if (stride_q < nq || stride_k < nk || stride_v < nk || stride_q % 8 || stride_k % 8 || stride_v % 8)
+        return fail(c, CC_ERR_SHAPE, "row strides must be multiples of 8 and cover a row");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out))
+        return fail(c, CC_ERR_SHAPE, "buffers must be 16-byte aligned");
+    if (q_out == q && stride_q != nq) return fail(c, CC_ERR_SHAPE, "q_out may be q only where q's rows are contiguous");
+    device_scope dev(c->device);
+    if (flags & CC_FLAG_CHECK_IDX) {
+        cc_status st = check_rows_sync(c, *rows, *pool, 0, 0, 1);
+        if (st != CC_OK) return st;
+    }
+    {
+        cc_prof_scope ps(c, CC_K_ROPE_APPEND);
+        cc_launch_rope_append((const bf16_t*)q, stride_q, (const bf16_t*)k, stride_k, (const bf16_t*)v, stride_v, *rows, pos, *pool,
+                              *kv, *rope, c->m, (bf16_t*)q_out, c->stream);
+    }
+    CC_HIP(c, hipGetLastError());
+    return CC_OK;
+}
+
+cc_status cc_step_paged_attention(cc_ctx* c, const void* q, const cc_new_rows* rows, const cc_page_pool* pool, const cc_paged_kv* kv,
+                                  int32_t window, int32_t sinks, void* o, int32_t flags) {
+    if (!c) return fail(nullptr, CC_ERR_NULL, "ctx must not be NULL");
+    CC_REFUSE(c, cc_check_pool(pool));
+    CC_REFUSE(c, cc_check_paged_kv(kv, pool->page_size, c->m.H_kv, c->m.d_h));
+    CC_REFUSE(c, cc_check_new_rows(rows, pool->n_seqs, c->m.H_q / c->m.H_kv));
+    if (rows->rows > 0 && (!q || !o)) return fail(c, CC_ERR_NULL, "q and o must not be NULL");
+    if (window < 0 || sinks < 0) return fail(c, CC_ERR_SHAPE, "window and sinks must be >= 0");
+    if (!aligned16(q) || !aligned16(o)) return fail(c, CC_ERR_SHAPE, "buffers must be 16-byte aligned");
+    device_scope dev(c->device);
+    if (flags & CC_FLAG_CHECK_IDX) {
+        cc_status st = check_rows_sync(c, *rows, *pool, window, sinks, 0);
+        if (st != CC_OK) return st;
+    }
+    {
+        cc_prof_scope ps(c, CC_K_PAGED_ATTN);
+        cc_launch_paged_attention((const bf16_t*)q, *rows, *pool, *kv, window, sinks, c->m, (bf16_t*)o, c->stream);
     }
     CC_HIP(c, hipGetLastError());
     return CC_OK;

@@ -1,0 +1,428 @@
+// Pages of the answer phase: growing, forking, freeing and compacting what sequences hold, the copies this
+// takes in every layer, and the rotary step that writes new keys and values into pages.
+//
+// The bookkeeping of a call is one workgroup's: its lists are short, every decision depends on a scan over them, and
+// what it costs is the latency of a few dependent passes.  Free pages are handed out lowest first in the order of the
+// list, so results do not depend on the order in which threads run; the only atomics add to counts.
+// The copies are left as a list in the pool's scratch and made by a second launch over all layers.
+#include "paged.h"
+
+namespace {
+
+constexpr int NT = 1024;
+
+// Inclusive scan over the workgroup; every thread comes here.  part: NT / 64 entries of LDS.
+template <class T>
+__device__ __forceinline__ T block_scan(T v, T* part, T& total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int off = 1; off < 64; off <<= 1) {
+        const T u = __shfl_up(v, off);
+        if (lane >= off) v += u;
+    }
+    __syncthreads();                                  // the last scan's part has been read
+    if (lane == 63) part[w] = v;
+    __syncthreads();
+    T base = 0, sum = 0;
+    for (int i = 0; i < NT / 64; ++i) {
+        if (i < w) base += part[i];
+        sum += part[i];
+    }
+    total = sum;
+    return base + v;
+}
+
+enum { BAD_INDEX = 1, BAD_LENGTH = 2, NO_PAGES = 4 };
+__device__ __forceinline__ void finish(int32_t* status, int32_t* host, int bad) {
+    if (threadIdx.x) return;
+    const int st = bad & BAD_INDEX ? CC_ERR_IDX : bad & BAD_LENGTH ? CC_ERR_SHAPE : bad & NO_PAGES ? CC_ERR_WORKSPACE : CC_OK;
+    *status = st;
+    if (host) *host = st;
+}
+
+// Sets BAD_INDEX where an index is out of range or repeated.  All threads; ends with a barrier.
+__device__ __forceinline__ void check_distinct(const int32_t* seq, int n, int n_seqs, int32_t* mark, int* bad) {
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const int s = seq[i];
+        if ((unsigned)s < (unsigned)n_seqs) mark[s] = 0;
+        else atomicOr(bad, BAD_INDEX);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const int s = seq[i];
+        if ((unsigned)s < (unsigned)n_seqs && atomicAdd(&mark[s], 1)) atomicOr(bad, BAD_INDEX);
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t* __restrict__ seq,
+                                                  const int32_t* __restrict__ n_new, int n, int32_t* work, cc_page_work w,
+                                                  int32_t* status, int32_t* host) {
+    __shared__ int bad;
+    __shared__ int64_t part[NT / 64];
+    const int tid = threadIdx.x, page = 1 << p.shift;
+    if (tid == 0) bad = 0, work[0] = 0;
+    __syncthreads();
+    check_distinct(seq, n, p.n_seqs, work + w.mark, &bad);
+    if (!(bad & BAD_INDEX))
+        for (int i = tid; i < n; i += NT) {
+            const int s = seq[i], c = n_new[i], L = p.len[s];
+            const int64_t to = (int64_t)L + c;
+            if (c < 0 || L < 0) { atomicOr(&bad, BAD_INDEX); continue; }
+            if (to > (int64_t)p.max_pages << p.shift) { atomicOr(&bad, BAD_LENGTH); continue; }
+            const int have = (L + page - 1) >> p.shift;
+            int copy = 0;
+            if (c > 0 && (L & (page - 1))) {
+                const int last = p.table[s * p.st_table + have - 1];
+                if ((unsigned)last >= (unsigned)p.n_pages) { atomicOr(&bad, BAD_INDEX); continue; }
+                copy = p.refs[last] > 1;
+            }
+            work[w.take + i] = 2 * ((int)((to + page - 1) >> p.shift) - have + copy) + copy;
+        }
+    __syncthreads();
+    if (bad) return finish(status, host, bad);
+
+    // pages taken and copies made before entry i (copies in the upper half of a 64-bit sum)
+    int64_t carry = 0;
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + tid;
+        const int t = i < n ? work[w.take + i] : 0;
+        const int64_t mine = (t >> 1) + ((int64_t)(t & 1) << 40);
+        int64_t sum;
+        const int64_t before = carry + block_scan(mine, part, sum) - mine;
+        if (i < n) {
+            work[w.first + i] = (int)min(before & ((1ll << 40) - 1), (int64_t)1 << 30);
+            work[w.copy_at + i] = (int)(before >> 40);
+        }
+        carry += sum;
+    }
+    const int64_t total = carry & ((1ll << 40) - 1);
+    const int copies = (int)(carry >> 40);
+
+    // the lowest free pages, eight consecutive pages a thread and step, until there are enough
+    constexpr int PER = 8;
+    int64_t found = 0;
+    for (int64_t p0 = 0; p0 < p.n_pages && found < total; p0 += NT * PER) {
+        const int64_t a = p0 + (int64_t)tid * PER;
+        unsigned free = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (a + k < p.n_pages && p.refs[a + k] == 0) free |= 1u << k;
+        int64_t sum;
+        int64_t at = found + block_scan((int64_t)__popc(free), part, sum) - __popc(free);
+        for (; free; free &= free - 1, ++at)
+            if (at < total) work[w.list + at] = (int)(a + __ffs(free) - 1);
+        found += sum;
+    }
+    __syncthreads();
+    if (found < total) return finish(status, host, NO_PAGES);
+
+    const int lane = tid & 63;
+    for (int i = tid >> 6; i < n; i += NT / 64) {             // a wave per entry
+        const int s = seq[i], c = n_new[i], L = p.len[s], copy = work[w.take + i] & 1;
+        const int have = (L + page - 1) >> p.shift, fresh = (work[w.take + i] >> 1) - copy;
+        int32_t* row = p.table + s * p.st_table;
+        const int32_t* mine = work + w.list + work[w.first + i];
+        if (copy && lane == 0) {
+            const int k = work[w.copy_at + i], old = row[have - 1];
+            work[w.src + k] = old;
+            work[w.dst + k] = mine[0];
+            work[w.rows + k] = L & (page - 1);
+            atomicSub(&p.refs[old], 1);
+            p.refs[mine[0]] = 1;
+            row[have - 1] = mine[0];
+        }
+        for (int k = lane; k < fresh; k += 64) {
+            const int q = mine[copy + k];
+            row[have + k] = q;
+            p.refs[q] = 1;
+        }
+        if (lane == 0) p.len[s] = L + c;
+    }
+    if (tid == 0) work[0] = copies;
+    finish(status, host, 0);
+}
+
+__global__ __launch_bounds__(NT) void fork_kernel(cc_pool_view p, const int32_t* __restrict__ src,
+                                                  const int32_t* __restrict__ dst, int n, int32_t* work, cc_page_work w,
+                                                  int32_t* status, int32_t* host) {
+    __shared__ int bad;
+    const int tid = threadIdx.x, page = 1 << p.shift;
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    check_distinct(dst, n, p.n_seqs, work + w.mark, &bad);
+    for (int i = tid; i < n; i += NT) {
+        const int s = src[i], d = dst[i];
+        if ((unsigned)s >= (unsigned)p.n_seqs || ((unsigned)d < (unsigned)p.n_seqs && p.len[d] != 0)) atomicOr(&bad, BAD_INDEX);
+        else work[w.take + i] = cc_seq_len(p, s);             // as it is at the call
+    }
+    __syncthreads();
+    if (bad) return finish(status, host, bad);
+    const int lane = tid & 63;
+    for (int i = tid >> 6; i < n; i += NT / 64) {
+        const int L = work[w.take + i], held = (L + page - 1) >> p.shift;
+        const int32_t* from = p.table + src[i] * p.st_table;
+        int32_t* to = p.table + dst[i] * p.st_table;
+        for (int c = lane; c < held; c += 64) {
+            const int q = from[c];
+            to[c] = q;
+            if ((unsigned)q < (unsigned)p.n_pages) atomicAdd(&p.refs[q], 1);
+        }
+        if (lane == 0) p.len[dst[i]] = L;
+    }
+    finish(status, host, 0);
+}
+
+__global__ __launch_bounds__(NT) void free_kernel(cc_pool_view p, const int32_t* __restrict__ seq, int n, int32_t* work,
+                                                  cc_page_work w, int32_t* status, int32_t* host) {
+    __shared__ int bad;
+    const int tid = threadIdx.x, page = 1 << p.shift;
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    check_distinct(seq, n, p.n_seqs, work + w.mark, &bad);
+    if (bad) return finish(status, host, bad);
+    const int lane = tid & 63;
+    for (int i = tid >> 6; i < n; i += NT / 64) {
+        const int s = seq[i], held = (cc_seq_len(p, s) + page - 1) >> p.shift;
+        int32_t* row = p.table + s * p.st_table;
+        for (int c = lane; c < held; c += 64) {
+            const int q = row[c];
+            row[c] = -1;
+            if ((unsigned)q < (unsigned)p.n_pages) atomicSub(&p.refs[q], 1);
+        }
+        if (lane == 0) p.len[s] = 0;
+    }
+    finish(status, host, 0);
+}
+
+// Which page goes where: the i-th used page at L or behind to the i-th free one in front of L.
+__global__ __launch_bounds__(NT) void compact_plan_kernel(cc_pool_view p, int32_t* work, cc_page_work w, int32_t* status,
+                                                          int32_t* host) {
+    __shared__ int part[NT / 64];
+    constexpr int PER = 8;
+    const int tid = threadIdx.x;
+    int mine = 0, live;
+    for (int64_t a = tid; a < p.n_pages; a += NT) mine += p.refs[a] != 0;
+    block_scan(mine, part, live);
+    int holes = 0, movers = 0;
+    for (int64_t p0 = 0; p0 < p.n_pages; p0 += NT * PER) {
+        const int64_t a = p0 + (int64_t)tid * PER;
+        unsigned hole = 0, move = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (a + k < p.n_pages) {
+                const bool used = p.refs[a + k] != 0;
+                if (a + k < live ? !used : used) (a + k < live ? hole : move) |= 1u << k;
+            }
+        int sum;
+        // holes in the low half of the sum, movers in the high one (at most 8192 of each a step)
+        const int cnt = __popc(hole) + (__popc(move) << 16);
+        const int before = block_scan(cnt, part, sum) - cnt;
+        int h = holes + (before & 0xffff), m = movers + (before >> 16);
+        for (; hole; hole &= hole - 1) work[w.dst + h++] = (int)(a + __ffs(hole) - 1);
+        for (; move; move &= move - 1) work[w.src + m++] = (int)(a + __ffs(move) - 1);
+        holes += sum & 0xffff;
+        movers += sum >> 16;
+    }
+    __syncthreads();
+    for (int i = tid; i < movers; i += NT) {
+        const int from = work[w.src + i], to = work[w.dst + i];
+        work[w.map + from] = to;
+        work[w.rows + i] = 1 << p.shift;
+        p.refs[to] = p.refs[from];
+        p.refs[from] = 0;
+    }
+    if (tid == 0) {
+        work[0] = movers;
+        work[1] = live;
+    }
+    finish(status, host, 0);
+}
+
+// Entries of every sequence that name a moved page; a wave per sequence.
+__global__ __launch_bounds__(256) void compact_table_kernel(cc_pool_view p, const int32_t* __restrict__ work, cc_page_work w) {
+    const int s = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, live = work[1];
+    if (s >= p.n_seqs) return;
+    const int held = (cc_seq_len(p, s) + (1 << p.shift) - 1) >> p.shift;
+    int32_t* row = p.table + s * p.st_table;
+    for (int c = lane; c < held; c += 64) {
+        const int q = row[c];
+        if (q >= live && q < p.n_pages) row[c] = work[w.map + q];
+    }
+}
+
+struct copy_args {
+    void* ptr[2 * CC_PAGE_LAYERS];
+    int32_t n_ptr;
+};
+// A workgroup takes a (copy, tensor) at a time: the copy's rows of all heads, 16 bytes a lane.
+template <int D_H>
+__global__ __launch_bounds__(256) void page_copy_kernel(copy_args a, const int32_t* __restrict__ work, cc_page_work w,
+                                                        int H_kv, int64_t st_page, int64_t st_tok, int64_t st_head) {
+    constexpr int CPH = D_H / 8;
+    const int64_t items = (int64_t)work[0] * a.n_ptr;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int i = (int)(it / a.n_ptr), t = (int)(it - (int64_t)i * a.n_ptr);
+        const int rows = work[w.rows + i], units = rows * H_kv * CPH;
+        bf16_t* base = (bf16_t*)a.ptr[t];
+        const bf16_t* from = base + work[w.src + i] * st_page;
+        bf16_t* to = base + work[w.dst + i] * st_page;
+        for (int u = threadIdx.x; u < units; u += 256) {
+            const int c = u % CPH, r = u / CPH;
+            const int tok = st_tok > st_head ? r / H_kv : r % rows, h = st_tok > st_head ? r % H_kv : r / rows;
+            const int64_t at = tok * st_tok + h * st_head + c * 8;
+            *reinterpret_cast<u32x4*>(to + at) = *reinterpret_cast<const u32x4*>(from + at);
+        }
+    }
+}
+
+__global__ __launch_bounds__(64) void check_rows_kernel(const int32_t* __restrict__ start, const int32_t* __restrict__ seq, int rows,
+                                                        cc_pool_view p, int window, int sinks, int append, int32_t* flag) {
+    const int b = blockIdx.x, lane = threadIdx.x, r0 = start[b], r1 = start[b + 1], s = seq ? seq[b] : b;
+    bool bad = r0 < 0 || r1 < r0 || r1 > rows || (unsigned)s >= (unsigned)p.n_seqs;
+    if (!bad) {
+        const int n = r1 - r0, L = p.len[s];
+        bad = L < n || L > (int64_t)p.max_pages << p.shift;
+        if (!bad && n > 0) {
+            const int first = L - n;
+            const int low = append ? first : window > 0 ? max(0, first - window + 1) : 0;
+            const int seen = append ? 0 : min(low, sinks);
+            for (int c = lane; c <= (L - 1) >> p.shift; c += 64)
+                if ((c >= low >> p.shift || c << p.shift < seen) && (unsigned)p.table[s * p.st_table + c] >= (unsigned)p.n_pages) bad = true;
+        }
+    }
+    if (__any(bad) && lane == 0) *flag = 1;
+}
+
+struct rope_args {
+    double turns[64];           // of pair j per position
+    int32_t rot, interleaved;
+    float mscale;
+};
+// A wave per row.  The row's (cos, sin) are computed once: the angle in turns in 64 bits (a far position's angle keeps
+// its fraction), its fraction's sine and cosine in 32.  A lane owns 16 bytes of a head and reads the pairs' other members
+// from where they lie; all loads of a head come before its stores, so queries may be turned in place.
+template <int D_H>
+__global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf16_t* q, int64_t st_q, const bf16_t* __restrict__ k,
+                                                          int64_t st_k, const bf16_t* __restrict__ v, int64_t st_v,
+                                                          const int32_t* __restrict__ start, const int32_t* __restrict__ seq, int n,
+                                                          int rows, const int32_t* __restrict__ pos, cc_pool_view p, bf16_t* Kp,
+                                                          bf16_t* Vp, int64_t st_page, int64_t st_tok, int64_t st_head, int H_q,
+                                                          int H_kv, bf16_t* q_out) {
+    constexpr int CPH = D_H / 8;
+    __shared__ float2 cs[4][64];
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int r = blockIdx.x * 4 + w;
+    const int b = r < rows ? cc_row_owner(start, n, r) : -1;
+    int at = -1, page = -1;
+    if (b >= 0) {
+        const int s = seq ? seq[b] : b;
+        const int L = cc_seq_len(p, s);
+        at = L - start[b + 1] + r;
+        if (at >= 0 && at < L) page = p.table[s * p.st_table + (at >> p.shift)];
+        else at = -1;
+    }
+    const int half = a.rot / 2;
+    if (at >= 0 && lane < half) {
+        const double x = (double)(pos ? pos[r] : at) * a.turns[lane];
+        float sn, c;
+        sincospif(2.0f * (float)(x - rint(x)), &sn, &c);
+        cs[w][lane] = make_float2(c * a.mscale, sn * a.mscale);
+    }
+    __syncthreads();
+    if (at < 0) return;
+    const bool stored = (unsigned)page < (unsigned)p.n_pages;
+    const int64_t slot = stored ? page * st_page + (int64_t)(at & ((1 << p.shift) - 1)) * st_tok : 0;
+    for (int u = lane; u < (H_q + 2 * H_kv) * CPH; u += 64) {
+        const int h = u / CPH, e0 = u % CPH * 8;
+        const int hk = h - H_q, hv = hk - H_kv;
+        if (hk >= 0 && !stored) continue;
+        const bf16_t* src = hk < 0 ? q + r * st_q + h * D_H : hv < 0 ? k + r * st_k + hk * D_H : v + r * st_v + hv * D_H;
+        bf16_t* dst = hk < 0 ? q_out + ((int64_t)r * H_q + h) * D_H : (hv < 0 ? Kp + slot + hk * st_head : Vp + slot + hv * st_head);
+        bf16_t x[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = src[e0 + e];
+        if (hv < 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = e0 + e;
+                const int other = i >= a.rot ? i : a.interleaved ? i ^ 1 : i < half ? i + half : i - half;
+                y[e] = src[other];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = e0 + e;
+                if (i >= a.rot) continue;
+                const float2 c = cs[w][a.interleaved ? i >> 1 : i < half ? i : i - half];
+                const bool first = a.interleaved ? (i & 1) == 0 : i < half;
+                const float m = (float)x[e] * c.x, o = (float)y[e] * c.y;
+                x[e] = (bf16_t)(first ? m - o : m + o);
+            }
+        }
+        bf16x8 out;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = x[e];
+        *reinterpret_cast<bf16x8*>(dst + e0) = out;
+    }
+}
+
+}  // namespace
+
+void cc_launch_grow(const cc_page_pool& p, const int32_t* seq, const int32_t* n_new, int n, int32_t* host, hipStream_t s) {
+    hipLaunchKernelGGL(grow_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), seq, n_new, n, (int32_t*)p.work,
+                       cc_page_work_layout(p.n_pages, p.n_seqs), p.status, host);
+}
+void cc_launch_fork(const cc_page_pool& p, const int32_t* src, const int32_t* dst, int n, int32_t* host, hipStream_t s) {
+    hipLaunchKernelGGL(fork_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), src, dst, n, (int32_t*)p.work,
+                       cc_page_work_layout(p.n_pages, p.n_seqs), p.status, host);
+}
+void cc_launch_free(const cc_page_pool& p, const int32_t* seq, int n, int32_t* host, hipStream_t s) {
+    hipLaunchKernelGGL(free_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), seq, n, (int32_t*)p.work,
+                       cc_page_work_layout(p.n_pages, p.n_seqs), p.status, host);
+}
+void cc_launch_compact(const cc_page_pool& p, int32_t* host, hipStream_t s) {
+    const cc_page_work w = cc_page_work_layout(p.n_pages, p.n_seqs);
+    hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), (int32_t*)p.work, w, p.status, host);
+    hipLaunchKernelGGL(compact_table_kernel, dim3((p.n_seqs + 3) / 4), dim3(256), 0, s, cc_view(p), (const int32_t*)p.work, w);
+}
+
+void cc_launch_page_copies(const cc_page_pool& p, const cc_paged_kv* kv, int n_layers, int most, int H_kv, int d_h, hipStream_t s) {
+    const cc_page_work w = cc_page_work_layout(p.n_pages, p.n_seqs);
+    for (int l0 = 0; l0 < n_layers; l0 += CC_PAGE_LAYERS) {
+        copy_args a;
+        a.n_ptr = 2 * std::min(CC_PAGE_LAYERS, n_layers - l0);
+        for (int i = 0; i < a.n_ptr; ++i) a.ptr[i] = i & 1 ? kv[l0 + i / 2].V : kv[l0 + i / 2].K;
+        const dim3 grid((unsigned)std::min<int64_t>((int64_t)most * a.n_ptr, 8 * cc_device_cus()));
+        if (grid.x == 0) return;
+        if (d_h == 128)
+            hipLaunchKernelGGL(page_copy_kernel<128>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, kv[0].stride_page,
+                               kv[0].stride_token, kv[0].stride_head);
+        else
+            hipLaunchKernelGGL(page_copy_kernel<64>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, kv[0].stride_page,
+                               kv[0].stride_token, kv[0].stride_head);
+    }
+}
+
+void cc_launch_check_rows(const cc_new_rows& r, const cc_page_pool& p, int window, int sinks, int append, int32_t* flag, hipStream_t s) {
+    if (r.n > 0)
+        hipLaunchKernelGGL(check_rows_kernel, dim3(r.n), dim3(64), 0, s, r.start, r.seq, r.rows, cc_view(p), window, sinks, append, flag);
+}
+
+void cc_launch_rope_append(const bf16_t* q, int64_t st_q, const bf16_t* k, int64_t st_k, const bf16_t* v, int64_t st_v,
+                           const cc_new_rows& r, const int32_t* pos, const cc_page_pool& p, const cc_paged_kv& kv,
+                           const cc_rope& rope, const cc_model_desc& m, bf16_t* q_out, hipStream_t s) {
+    if (r.rows <= 0 || r.n <= 0) return;
+    rope_args a;
+    cc_rope_turns(rope, a.turns);
+    a.rot = rope.rot;
+    a.interleaved = rope.interleaved != 0;
+    a.mscale = (float)rope.mscale;
+    const dim3 grid((r.rows + 3) / 4);
+    if (m.d_h == 128)
+        hipLaunchKernelGGL(rope_append_kernel<128>, grid, dim3(256), 0, s, a, q, st_q, k, st_k, v, st_v, r.start, r.seq, r.n, r.rows,
+                           pos, cc_view(p), (bf16_t*)kv.K, (bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, m.H_q,
+                           m.H_kv, q_out);
+    else
+        hipLaunchKernelGGL(rope_append_kernel<64>, grid, dim3(256), 0, s, a, q, st_q, k, st_k, v, st_v, r.start, r.seq, r.n, r.rows,
+                           pos, cc_view(p), (bf16_t*)kv.K, (bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, m.H_q,
+                           m.H_kv, q_out);
+}
