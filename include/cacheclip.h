@@ -312,7 +312,7 @@ typedef struct cc_paged_kv {
 typedef struct cc_new_rows {
     const int32_t* start;   /* dev [n + 1], ascending, within [0, rows] */
     const int32_t* seq;     /* dev [n], each in [0, n_seqs), or NULL */
-    int32_t n;              /* sequences, 0 to 2048 */
+    int32_t n;              /* sequences, 0 to 1024 */
     int32_t rows;           /* rows of the buffers */
     int32_t max_new;        /* most rows of any sequence, as a bound: it only decides launch shapes */
 } cc_new_rows;

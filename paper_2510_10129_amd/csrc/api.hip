@@ -193,7 +193,7 @@ cc_status cc_create(cc_ctx** out, const cc_model_desc* desc, void* hip_stream) {
     memset(c->prof_ms, 0, sizeof(c->prof_ms));
     memset(c->prof_n, 0, sizeof(c->prof_n));
     c->rope = nullptr; c->xn = nullptr; c->q = nullptr; c->o = nullptr; c->y = nullptr;
-    c->mn = nullptr; c->act = nullptr; c->attn_part = nullptr; c->attn_table = nullptr; c->gemm_part = nullptr; c->score = nullptr; c->key_range = nullptr; c->sel = nullptr; c->n_sel = nullptr; c->flag = nullptr;
+    c->mn = nullptr; c->act = nullptr; c->attn_part = nullptr; c->attn_table = nullptr; c->gemm_part = nullptr; c->score = nullptr; c->key_range = nullptr; c->sel = nullptr; c->n_sel = nullptr; c->flag = nullptr; c->paged = nullptr;
     c->pinned = c->pinned_dev = nullptr;
     const cc_model_desc& m = c->m;
     const size_t Mc = (size_t)m.M_cap, nq = (size_t)m.H_q * m.d_h;
@@ -231,6 +231,9 @@ cc_status cc_create(cc_ctx** out, const cc_model_desc* desc, void* hip_stream) {
     }
     alloc((void**)&c->n_sel, 4);
     alloc((void**)&c->flag, 4);
+    alloc((void**)&c->paged, CC_PAGED_CTX_INTS * sizeof(int32_t));
+    if (e == hipSuccess) e = hipMemset(c->paged, 0, CC_PAGED_CTX_INTS * sizeof(int32_t));
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);   // a stream of the caller's need not wait for the default one
     if (e == hipSuccess) e = hipHostMalloc((void**)&c->pinned, 4 * sizeof(int32_t), hipHostMallocDefault);
     if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->pinned_dev, c->pinned, 0);
     if (e != hipSuccess) {
@@ -257,7 +260,7 @@ cc_status cc_destroy(cc_ctx* c) {
     (void)hipFree(c->rope); (void)hipFree(c->xn); (void)hipFree(c->q); (void)hipFree(c->o);
     (void)hipFree(c->y); (void)hipFree(c->mn); (void)hipFree(c->act); (void)hipFree(c->attn_part); (void)hipFree(c->attn_table); (void)hipFree(c->gemm_part);
     (void)hipFree(c->score); (void)hipFree(c->key_range); (void)hipFree(c->sel);
-    (void)hipFree(c->n_sel); (void)hipFree(c->flag);
+    (void)hipFree(c->n_sel); (void)hipFree(c->flag); (void)hipFree(c->paged);
     if (c->pinned) (void)hipHostFree(c->pinned);
     delete c;
     return CC_OK;
@@ -723,7 +726,8 @@ cc_status cc_step_paged_attention(cc_ctx* c, const void* q, const cc_new_rows* r
     }
     {
         cc_prof_scope ps(c, CC_K_PAGED_ATTN);
-        cc_launch_paged_attention((const bf16_t*)q, *rows, *pool, *kv, window, sinks, c->m, (bf16_t*)o, c->stream);
+        cc_launch_paged_attention((const bf16_t*)q, *rows, *pool, *kv, window, sinks, c->m,
+                                  {(const bf16_t*)(c->paged + CC_PAGED_WGS), c->paged}, (bf16_t*)o, c->stream);
     }
     CC_HIP(c, hipGetLastError());
     return CC_OK;

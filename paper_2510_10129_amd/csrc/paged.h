@@ -41,5 +41,10 @@ void cc_launch_check_rows(const cc_new_rows& r, const cc_page_pool& p, int windo
 void cc_launch_rope_append(const bf16_t* q, int64_t st_q, const bf16_t* k, int64_t st_k, const bf16_t* v, int64_t st_v,
                            const cc_new_rows& r, const int32_t* pos, const cc_page_pool& p, const cc_paged_kv& kv,
                            const cc_rope& rope, const cc_model_desc& m, bf16_t* q_out, hipStream_t s);
+// Of the context: d_h zeros, and a count per workgroup that is zero between calls.
+struct cc_paged_scratch {
+    const bf16_t* zeros;
+    int32_t* arrived;
+};
 void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_page_pool& p, const cc_paged_kv& kv, int window,
-                               int sinks, const cc_model_desc& m, bf16_t* o, hipStream_t s);
+                               int sinks, const cc_model_desc& m, const cc_paged_scratch& ws, bf16_t* o, hipStream_t s);

@@ -1,79 +1,542 @@
 // Causal grouped-query attention of new rows over a paged cache, optionally under a sliding window with sinks.
+//
+// Few rows (few_attn_kernel).  A sequence's new rows are a handful of (row, query head) columns per kv head, every key and
+// value is read once, and what bounds the call is how fast HBM delivers them: 512 bytes a key and head at d_h = 128
+// against 4 d_h flops a column, 16 to 64 columns.  So the chip is filled along the keys: the key tiles of all
+// (sequence, kv head) blocks form one sequence of units that is cut into equal ranges, a workgroup each (one per CU), and a
+// block that a cut goes through is put together from its pieces by the workgroup that finishes it last.  Within a workgroup the
+// tiles of a block are dealt to four waves that run on their own: a wave keeps a ring of tiles of its own in LDS, filled by
+// 16-byte global->LDS loads, and waits for nothing but its own loads, so that 16 to 32 KB per wave, up to 128 KB per CU,
+// are always on their way.
+//
+// A wave computes S^T = K Q^T and O^T = V^T P^T with 16x16x32 MFMAs, columns on the N side: a lane then owns one
+// column, its scores are laid out as the second product's operand needs them, and the rescale factor is one number per
+// lane.  The running maximum moves only when a score exceeds it by more than 2^8 (in base 2), so most tiles need neither an
+// exchange between lanes nor a rescale; probabilities up to 2^8 in bf16 and sums in fp32 cancel in the final division.
 #include "paged.h"
+
+#include <type_traits>
 
 namespace {
 
-// A wave per (row, query head): 64 keys at a time, a lane per key for the scores, a lane per D_H / 64 elements for the
-// values, with the running maximum and sum of an online softmax.
-template <int D_H>
-__global__ __launch_bounds__(64) void row_attn_kernel(const bf16_t* __restrict__ q, const int32_t* __restrict__ start,
-                                                      const int32_t* __restrict__ seq, int n, int rows, cc_pool_view p,
-                                                      const bf16_t* __restrict__ Kp, const bf16_t* __restrict__ Vp, int64_t st_page,
-                                                      int64_t st_tok, int64_t st_head, int window, int sinks, int H_q, int H_kv,
-                                                      float scale_log2, bf16_t* __restrict__ o) {
-    constexpr int DL = D_H / 64;
-    __shared__ float qs[D_H], ps[64];
-    __shared__ int64_t slot[64];
-    const int lane = threadIdx.x, r = blockIdx.x, h = blockIdx.y, kvh = h / (H_q / H_kv);
-    const int b = cc_row_owner(start, n, r);
-    if (b < 0) return;
-    const int s = seq ? seq[b] : b, L = cc_seq_len(p, s), at = L - start[b + 1] + r;
-    const int64_t row = ((int64_t)r * H_q + h) * D_H;
-#pragma unroll
-    for (int e = 0; e < DL; ++e) qs[lane * DL + e] = (float)q[row + lane * DL + e];
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, acc[DL] = {};
-    const int low = window > 0 ? max(0, at - window + 1) : 0;
-    for (int j0 = 0; j0 <= at; j0 += 64) {
-        if (j0 + 63 < low && j0 >= sinks) continue;
-        const int j = j0 + lane;
-        bool on = j <= at && (j >= low || j < sinks);
-        int64_t a = -1;
-        float z = on ? 0.0f : -INFINITY;
-        if (on) {
-            const int page = p.table[s * p.st_table + (j >> p.shift)];
-            if ((unsigned)page < (unsigned)p.n_pages) {
-                a = page * st_page + (int64_t)(j & ((1 << p.shift) - 1)) * st_tok + kvh * st_head;
-                for (int e = 0; e < D_H; ++e) z += qs[e] * (float)Kp[a + e];
-                z *= scale_log2;
+constexpr int KEYS = 32;                      // of a tile of few_attn_kernel
+constexpr int WAVES = 4;
+constexpr int START = 4;                      // units that a block costs besides its tiles: its queries, first loads and result
+
+template <int NI, int I = 0, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < NI) {
+        f(std::integral_constant<int, I>{});
+        static_for<NI, I + 1>(f);
+    }
+}
+
+// 16 bytes per lane from global memory into LDS at wave base + OFF + 16 * lane; OFF is added to the global address too.
+template <int OFF>
+__device__ __forceinline__ void dma16(const char* gsrc_minus_off, char* lds_wave_base) {
+    static_assert(OFF >= 0 && OFF < 4096, "the instruction offset is 13 bits signed");
+    __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)gsrc_minus_off,
+                                     (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 0);
+}
+// LDS reads by hand: the compiler would wait for all loads into LDS before each.  Every read is issued and waited for in one
+// basic block.
+template <int IMM>
+__device__ __forceinline__ bf16x8 lds_read_b128(uint32_t addr) {
+    bf16x8 v;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(IMM));
+    return v;
+}
+// Transposing read: within 16 lanes, lane i receives as element e element i % 4 of the 8 bytes addressed by lane i / 4 + 4 e.
+template <int IMM>
+__device__ __forceinline__ bf16x4 lds_read_tr(uint32_t addr) {
+    bf16x4 v;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(IMM));
+    return v;
+}
+// At most N of this wave's loads from memory still on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+    asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return ((int64_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
+}
+
+// Key tiles of `keys` keys that the rows of a sequence see: the first `sink` tiles, then those from `from` to the end.
+struct tile_span {
+    int sink, from, count;
+    __device__ __forceinline__ int tile(int t) const { return t < sink ? t : t - sink + from; }
+};
+__device__ __forceinline__ tile_span visible_tiles(int first, int L, int window, int sinks, int keys) {
+    tile_span s;
+    const int low = window > 0 ? (int)max((int64_t)0, (int64_t)first - window + 1) : 0;
+    s.from = low / keys;
+    s.sink = window > 0 ? min((int)(((int64_t)sinks + keys - 1) / keys), s.from) : 0;
+    s.count = max(1, s.sink + (L + keys - 1) / keys - s.from);       // a row that sees nothing still has its zeros to write
+    return s;
+}
+
+struct paged_args {
+    const bf16_t* q;
+    bf16_t* o;
+    const int32_t* start;
+    const int32_t* seq;
+    int32_t n, rows;
+    cc_pool_view p;
+    const bf16_t* K;
+    const bf16_t* V;
+    int64_t st_page, st_tok, st_head;
+    int32_t window, sinks, H_q, H_kv, g;
+    float scale_log2;
+    const bf16_t* zeros;        // d_h of them
+    float* part;                // pieces: two slots a workgroup
+    int32_t* arrived;           // [workgroups], zero between calls
+};
+
+struct batch_seq {
+    int row0, n, s, L;          // first row, rows, row of the table, tokens
+};
+__device__ __forceinline__ batch_seq seq_of(const paged_args& a, int b) {
+    batch_seq r;
+    const int r0 = max(0, a.start[b]), r1 = min(a.rows, a.start[b + 1]);
+    r.row0 = r0;
+    r.n = max(0, r1 - r0);
+    r.s = a.seq ? a.seq[b] : b;
+    r.L = cc_seq_len(a.p, r.s);
+    if ((unsigned)r.s >= (unsigned)a.p.n_seqs) r.s = 0;
+    return r;
+}
+
+// NC: blocks of 16 columns that a wave multiplies a tile with.  Compiled for workgroups of eight waves, two a SIMD: with 512 registers the
+// compiler keeps the sums in accumulation registers and copies them out and in for every rescale.
+template <int D_H, int NC>
+__global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_min) {
+    constexpr int KS = D_H / 32;              // k-steps of the scores
+    constexpr int DT = D_H / 16;              // 16-row tiles of O^T
+    constexpr int CPR = D_H / 8;              // 16-byte chunks of a row
+    constexpr int RPI = 64 / CPR;             // rows moved by one load
+    constexpr int NL = KEYS / RPI;            // loads of a K or V tile
+    constexpr int HL = NL / 2;                // of 16 keys: within one page
+    constexpr int ROW = D_H * 2;              // bytes
+    constexpr int TILE = KEYS * ROW;
+    constexpr int NS = D_H == 128 ? 2 : 4;    // tiles in a wave's ring
+    constexpr int RING = 2 * NS * TILE;
+    constexpr int COLS = 16 * NC;
+    constexpr bool Q_LDS = NC * KS > 8;       // the queries' fragments do not fit the registers
+    __shared__ __align__(1024) char ring[WAVES][RING];
+    __shared__ int64_t pre[CC_PAGED_MAX_N + 1];
+    __shared__ int64_t wave_sum[WAVES];
+    __shared__ float2 ml[WAVES][COLS];
+    __shared__ bf16x8 qs[Q_LDS ? NC : 1][Q_LDS ? KS : 1][64];
+    __shared__ int last_here;
+    static_assert(COLS * D_H * 4 <= RING, "a wave's sums fit its ring");
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+    const int c16 = lane & 15, kg = lane >> 4;
+
+    // ---- units before every sequence of the batch ----
+    {
+        int64_t carry = 0;
+        for (int i0 = 0; i0 < a.n; i0 += 64 * WAVES) {
+            const int i = i0 + tid;
+            int64_t u = 0;
+            if (i < a.n) {
+                const batch_seq s = seq_of(a, i);
+                if (s.n > 0) {
+                    const tile_span v = visible_tiles(s.L - s.n, s.L, a.window, a.sinks, KEYS);
+                    u = (int64_t)((s.n * a.g + COLS - 1) / COLS) * a.H_kv * (v.count + START);
+                }
             }
+            int64_t inc = u;
+            for (int off = 1; off < 64; off <<= 1) {
+                const int64_t v = __shfl_up(inc, off);
+                if (lane >= off) inc += v;
+            }
+            if (lane == 63) wave_sum[w] = inc;
+            __syncthreads();
+            int64_t base = carry;
+            for (int j = 0; j < WAVES; ++j) {
+                if (j < w) base += wave_sum[j];
+                carry += wave_sum[j];
+            }
+            if (i < a.n) pre[i] = base + inc - u;
+            __syncthreads();
         }
-        float mx = z;
-        for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.0f : m_new;
-        const float pr = exp2f(z - ref), keep = exp2f(m - ref);
-        float sum = pr;
-        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-        l = l * keep + sum;
-        m = m_new;
-        ps[lane] = pr;
-        slot[lane] = a;
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < DL; ++e) acc[e] *= keep;
-        for (int i = 0; i < 64; ++i)
-            if (slot[i] >= 0)
-#pragma unroll
-                for (int e = 0; e < DL; ++e) acc[e] += ps[i] * (float)Vp[slot[i] + lane * DL + e];
+        if (tid == 0) pre[a.n] = carry;
         __syncthreads();
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const int64_t total = uniform(pre[a.n]);
+    const int64_t per = max((int64_t)per_min, (total + gridDim.x - 1) / gridDim.x);
+    const int range = blockIdx.x;
+    int64_t u = range * per;
+    const int64_t stop = min(u + per, total);
+
+    // ---- lane constants: loads (row and swizzled chunk) and fragment addresses ----
+    // K: chunk c of row r at slot c ^ kswz(r); V: the 32-byte pair of chunks dt at pair dt ^ vswz(r).
+    auto kswz = [](int r) { return D_H == 128 ? (r & 15) : ((r >> 1) & 7); };
+    auto vswz = [](int r) { return D_H == 128 ? (r & 7) : ((r >> 1) & 3); };
+    const int l_row = lane / CPR, l_c = lane % CPR;
+    uint32_t k_col[HL], v_col[HL];                        // byte within the row that load i of 16 keys fetches
 #pragma unroll
-    for (int e = 0; e < DL; ++e) o[row + lane * DL + e] = (bf16_t)(acc[e] * inv);
+    for (int i = 0; i < HL; ++i) {
+        const int r = i * RPI + l_row;
+        k_col[i] = (l_c ^ kswz(r)) * 16;
+        v_col[i] = (l_c ^ (2 * vswz(r))) * 16;
+    }
+    const uint32_t st_b = (uint32_t)a.st_tok * 2;
+    char* const my_ring = ring[w];
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)my_ring;
+    uint32_t kaddr[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kaddr[ks] = ring_at + c16 * ROW + (((ks * 4 + kg) ^ kswz(c16)) << 4);
+    const int v_row = 4 * kg + (c16 >> 2);
+    const uint32_t v_base = ring_at + TILE + v_row * ROW + ((((c16 & 3) >> 1) ^ (2 * vswz(v_row))) << 4) + (c16 & 1) * 8;
+    uint32_t vaddr[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vaddr[dt] = v_base ^ (dt << 5);
+
+    const uint32_t q_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)&qs[0][0][lane];
+
+    while (u < stop) {
+        // ---- the block that unit u lies in ----
+        int b = 0;
+        for (int i = lane; i - lane < a.n; i += 64) b += __popcll(__ballot(i < a.n && pre[min(i, a.n - 1) + 1] <= u));
+        b = uniform(b);
+        const batch_seq sq = seq_of(a, b);
+        const int row0 = uniform(sq.row0), n_new = uniform(sq.n), s = uniform(sq.s), L = uniform(sq.L);
+        const int first = L - n_new;
+        const tile_span span = visible_tiles(first, L, a.window, a.sinks, KEYS);
+        const int64_t seq0 = uniform(pre[b]);
+        const int len = span.count + START;
+        const int which = (int)((u - seq0) / len), blk = which / a.H_kv, h = which - blk * a.H_kv;
+        const int64_t u0 = seq0 + (int64_t)which * len, u1 = u0 + len;
+        const int ta = (int)max((int64_t)0, u - u0 - START), te = (int)(min(u1, stop) - u0 - START);
+        const bool opened_here = u0 + START >= range * per;
+        u = u1;
+        if (te <= ta) continue;
+
+        // ---- queries: B operand of the scores ----
+        bf16x8 qf[Q_LDS ? 1 : NC][KS];
+        int limit[NC], under[NC];                          // the newest key a column sees; keys up to `under` left its window
+        int most = -1, least = 0x7fffffff;                 // positions of the block's rows
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+            const int col = blk * COLS + nc * 16 + c16, i = col / a.g, hg = col - i * a.g;
+            const bool valid = i < n_new;
+            limit[nc] = valid ? max(first + i, -1) : -1;
+            under[nc] = a.window > 0 ? limit[nc] - a.window : (int)0x80000000;
+            most = max(most, limit[nc]);
+            if (valid) least = min(least, limit[nc]);
+            const bf16_t* qp = a.q + ((int64_t)(row0 + (valid ? i : 0)) * a.H_q + h * a.g + (valid ? hg : 0)) * D_H + 8 * kg;
+            if constexpr (Q_LDS) {
+                if (nc == w) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) qs[nc][ks][lane] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
+                }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) qf[nc][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
+            }
+        }
+        if constexpr (Q_LDS) __syncthreads();
+        for (int off = 8; off > 0; off >>= 1) {
+            most = max(most, __shfl_xor(most, off));
+            least = min(least, __shfl_xor(least, off));
+        }
+        most = uniform(most);
+        least = uniform(least);
+
+        f32x4 acc[DT][NC];
+        float m_run[NC], l_run[NC];
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+            m_run[nc] = -INFINITY;
+            l_run[nc] = 0.0f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[dt][nc] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // ---- loads of the wave's k-th tile ----
+        const int nt = te - ta > w ? (te - ta - w + WAVES - 1) / WAVES : 0;
+        auto tile_key = [&](int k) { return span.tile(ta + w + k * WAVES) * KEYS; };
+        // (constant for the launch: scalar loads, which do not count among the loads that the waits below count)
+        const __attribute__((address_space(4))) int32_t* row_table =
+            (const __attribute__((address_space(4))) int32_t*)(a.p.table + s * a.p.st_table);
+        const int64_t head_off = (int64_t)h * a.st_head;
+        // 16 keys from key0 on, in one page: its first row in K or V, or zeros for what no page holds
+        struct half_src { const char* k; const char* v; int rmax; };
+        auto half_of = [&](int key0) -> half_src {
+            half_src r;
+            const int page = key0 < L ? row_table[key0 >> a.p.shift] : -1;
+            if ((unsigned)page < (unsigned)a.p.n_pages) {
+                const int64_t at = (page * a.st_page + (int64_t)(key0 & ((1 << a.p.shift) - 1)) * a.st_tok + head_off) * 2;
+                r.k = (const char*)a.K + at;
+                r.v = (const char*)a.V + at;
+                r.rmax = min(15, L - 1 - key0);            // rows behind the last token repeat it (they are masked)
+            } else {
+                r.k = r.v = (const char*)a.zeros;
+                r.rmax = 0;
+            }
+            return r;
+        };
+        auto load = [&](const char* src, int rmax, const uint32_t* col, char* dst) __attribute__((always_inline)) {
+            static_for<HL>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                const uint32_t off = (uint32_t)min(i * RPI + l_row, rmax) * st_b + col[i];
+                dma16<i * 1024>(src - i * 1024 + off, dst);
+            });
+        };
+        auto load_k = [&](int k) __attribute__((always_inline)) {
+            const int key0 = tile_key(k);
+            char* dst = my_ring + (k % NS) * 2 * TILE;
+            const half_src x = half_of(key0), y = half_of(key0 + 16);
+            load(x.k, x.rmax, k_col, dst);
+            load(y.k, y.rmax, k_col, dst + TILE / 2);
+        };
+        auto load_v = [&](int k) __attribute__((always_inline)) {
+            const int key0 = tile_key(k);
+            char* dst = my_ring + (k % NS) * 2 * TILE + TILE;
+            const half_src x = half_of(key0), y = half_of(key0 + 16);
+            load(x.v, x.rmax, v_col, dst);
+            load(y.v, y.rmax, v_col, dst + TILE / 2);
+        };
+        for (int k = 0; k < NS && k < nt; ++k) {
+            load_k(k);
+            load_v(k);
+        }
+        // Loads younger than K(k): V(k) and the pairs of up to NS - 1 later tiles; than V(k): those and K(k + NS).
+        auto wait_k = [&](int rem) __attribute__((always_inline)) {
+            static_for<NS>([&](auto jc) __attribute__((always_inline)) {
+                constexpr int j = decltype(jc)::value;
+                if (j == NS - 1 ? rem >= j : rem == j) wait_loads<NL * (1 + 2 * j)>();
+            });
+        };
+        auto wait_v = [&](int rem) __attribute__((always_inline)) {
+            static_for<NS>([&](auto jc) __attribute__((always_inline)) {
+                constexpr int j = decltype(jc)::value;
+                if (rem == j) wait_loads<NL * 2 * j>();
+            });
+            if (rem >= NS) wait_loads<NL * (2 * (NS - 1) + 1)>();
+        };
+
+        for (int k = 0; k < nt; ++k) {
+            const int key0 = tile_key(k), rem = nt - 1 - k;
+            const uint32_t stage = (uint32_t)(k % NS) * 2 * TILE;
+            wait_k(rem);
+            bf16x8 kf[2][KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                kf[0][ks] = lds_read_b128<0>(kaddr[ks] + stage);
+                kf[1][ks] = lds_read_b128<16 * ROW>(kaddr[ks] + stage);
+            }
+            if constexpr (KS == 4)
+                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1]), "+v"(kf[0][2]),
+                             "+v"(kf[1][2]), "+v"(kf[0][3]), "+v"(kf[1][3])
+                             :: "memory");
+            else
+                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1])::"memory");
+            if (rem >= NS) load_k(k + NS);
+            f32x4 sc[NC][2];
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc) {
+                if constexpr (Q_LDS) {
+                    static_assert(!Q_LDS || KS == 4, "four fragments a column block");
+                    const uint32_t at = q_at + nc * KS * 1024;
+                    qf[0][0] = lds_read_b128<0>(at);
+                    qf[0][1] = lds_read_b128<1024>(at);
+                    qf[0][KS - 2] = lds_read_b128<(KS - 2) * 1024>(at);
+                    qf[0][KS - 1] = lds_read_b128<(KS - 1) * 1024>(at);
+                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(qf[0][0]), "+v"(qf[0][1]), "+v"(qf[0][KS - 2]), "+v"(qf[0][KS - 1]));
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    sc[nc][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+                        sc[nc][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][ks], qf[Q_LDS ? 0 : nc][ks], sc[nc][t], 0, 0, 0);
+                }
+            }
+            // ---- mask: keys behind a row, or in front of its window and no sink ----
+            if (key0 + KEYS - 1 > least || (a.window > 0 && key0 <= most - a.window && key0 + KEYS > a.sinks)) {
+#pragma unroll
+                for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int key = key0 + t * 16 + 4 * kg + v;
+                            // (no short circuits: selects, not branches)
+                            const bool out = (key > limit[nc]) | ((key <= under[nc]) & (key >= a.sinks));
+                            sc[nc][t][v] = out ? -INFINITY : sc[nc][t][v];
+                        }
+            }
+            // ---- softmax in base 2, the scale folded into the exponent ----
+            bf16x8 pf[NC];
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[nc][t][v]);
+                mx *= a.scale_log2;
+                if (__any(mx > m_run[nc] + 8.0f)) {
+                    mx = fmaxf(mx, __shfl_xor(mx, 16));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32));
+                    const float m_new = mx > m_run[nc] + 8.0f ? mx : m_run[nc];
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[nc] - (m_new == -INFINITY ? 0.0f : m_new));
+                    l_run[nc] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) acc[dt][nc] *= alpha;
+                    m_run[nc] = m_new;
+                }
+                const float ref = m_run[nc] == -INFINITY ? 0.0f : m_run[nc];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[nc][t][v], a.scale_log2, -ref));
+                        l_run[nc] += p;
+                        pf[nc][t * 4 + v] = (bf16_t)p;
+                    }
+            }
+            // ---- O^T += V^T P^T: the 32 keys in the order in which a lane holds its scores ----
+            wait_v(rem);
+            bf16x4 va[DT], vb[DT];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                va[dt] = lds_read_tr<0>(vaddr[dt] + stage);
+                vb[dt] = lds_read_tr<16 * ROW>(vaddr[dt] + stage);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(vb[0]), "+v"(va[1]), "+v"(vb[1]), "+v"(va[2]), "+v"(vb[2]),
+                         "+v"(va[3]), "+v"(vb[3])
+                         :: "memory");
+            if constexpr (DT == 8)
+                asm volatile("" : "+v"(va[4]), "+v"(vb[4]), "+v"(va[5]), "+v"(vb[5]), "+v"(va[6]), "+v"(vb[6]), "+v"(va[7]), "+v"(vb[7])::"memory");
+            if (rem >= NS) load_v(k + NS);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const bf16x8 vf = __builtin_shufflevector(va[dt], vb[dt], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int nc = 0; nc < NC; ++nc)
+                    acc[dt][nc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nc], acc[dt][nc], 0, 0, 0);
+            }
+        }
+
+        // ---- the four waves' sums together: as the registers lie, [dt][nc][lane] ----
+        wait_loads<0>();
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+            float l = l_run[nc];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (kg == 0) ml[w][nc * 16 + c16] = make_float2(m_run[nc], l);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                *reinterpret_cast<f32x4*>(my_ring + ((dt * NC + nc) * 64 + lane) * 16) = acc[dt][nc];
+        }
+        __syncthreads();
+        const bool whole = ta == 0 && te == span.count;
+        // pieces: a range leaves at most two, of the block it starts in and of a later one
+        float* const piece = a.part + (int64_t)(2 * range + (opened_here ? 1 : 0)) * COLS * (D_H + 2);
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+            float2 x[WAVES];
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int j = 0; j < WAVES; ++j) {
+                x[j] = ml[j][nc * 16 + c16];
+                m = fmaxf(m, x[j].x);
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int j = 0; j < WAVES; ++j) {
+                x[j].x = __builtin_amdgcn_exp2f(x[j].x - ref);
+                l += x[j].x * x[j].y;
+            }
+            const int col = blk * COLS + nc * 16 + c16, i = col / a.g, hg = col - i * a.g;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            for (int dt = w; dt < DT; dt += WAVES) {
+                f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < WAVES; ++j)
+                    r += x[j].x * *reinterpret_cast<const f32x4*>(ring[j] + ((dt * NC + nc) * 64 + lane) * 16);
+                if (!whole) {
+                    *reinterpret_cast<f32x4*>(piece + ((dt * NC + nc) * 64 + lane) * 4) = r;
+                } else if (i < n_new) {
+                    bf16x4 out;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[e] = (bf16_t)(r[e] * inv);
+                    *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * kg) = out;
+                }
+            }
+            if (!whole && w == 0 && kg == 0) *reinterpret_cast<float2*>(piece + COLS * D_H + (nc * 16 + c16) * 2) = make_float2(m, l);
+        }
+        if (whole) {
+            __syncthreads();                               // the rings are free again
+            continue;
+        }
+        // ---- a cut block: the workgroup that comes last adds the pieces, in the order of their keys ----
+        const int w0 = (int)((u0 + START) / per), w1 = (int)((u1 - 1) / per);
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+            last_here = before == w1 - w0;
+            if (last_here) __hip_atomic_store(&a.arrived[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last_here) continue;
+        __threadfence();
+        for (int e = tid; e < DT * NC * 64; e += 64 * WAVES) {
+            const int ln = e & 63, dn = e >> 6, nc = dn % NC, dt = dn / NC;
+            const int cc = nc * 16 + (ln & 15), col = blk * COLS + cc, i = col / a.g, hg = col - i * a.g;
+            if (i >= n_new) continue;
+            float m = -INFINITY, l = 0.0f;
+            f32x4 r = {0.f, 0.f, 0.f, 0.f};
+            for (int j = w0; j <= w1; ++j) {
+                const float* pc = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * COLS * (D_H + 2);
+                const float2 x = *reinterpret_cast<const float2*>(pc + COLS * D_H + cc * 2);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(pc + e * 4);
+                const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.0f : mn;
+                const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(x.x - ref);
+                l = l * keep + x.y * f;
+                r = r * keep + v * f;
+                m = mn;
+            }
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            bf16x4 out;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] = (bf16_t)(r[k] * inv);
+            *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * (ln >> 4)) = out;
+        }
+    }
 }
 
 }  // namespace
 
 void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_page_pool& p, const cc_paged_kv& kv, int window,
-                               int sinks, const cc_model_desc& m, bf16_t* o, hipStream_t s) {
+                               int sinks, const cc_model_desc& m, const cc_paged_scratch& ws, bf16_t* o, hipStream_t s) {
     if (r.rows <= 0 || r.n <= 0) return;
-    const float scale_log2 = 1.4426950408889634f / sqrtf((float)m.d_h);
-    const dim3 grid(r.rows, m.H_q);
-#define CC_ROW_ATTN(D)                                                                                                     \
-    hipLaunchKernelGGL(row_attn_kernel<D>, grid, dim3(64), 0, s, q, r.start, r.seq, r.n, r.rows, cc_view(p),               \
-                       (const bf16_t*)kv.K, (const bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, window, \
-                       sinks, m.H_q, m.H_kv, scale_log2, o)
-    if (m.d_h == 128) CC_ROW_ATTN(128);
-    else CC_ROW_ATTN(64);
-#undef CC_ROW_ATTN
+    const int g = m.H_q / m.H_kv;
+    paged_args a = {q, o, r.start, r.seq, r.n, r.rows, cc_view(p), (const bf16_t*)kv.K, (const bf16_t*)kv.V, kv.stride_page,
+                    kv.stride_token, kv.stride_head, window, sinks, m.H_q, m.H_kv, g,
+                    1.4426950408889634f / sqrtf((float)m.d_h), ws.zeros,
+                    (float*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn, ws.arrived};
+    const int grid = std::min(cc_device_cus(), CC_PAGED_WGS);
+    const int64_t columns = (int64_t)std::min(r.max_new, r.rows) * g;
+    const int per_min = 2 * WAVES + START;
+#define CC_FEW(D, NC) hipLaunchKernelGGL((few_attn_kernel<D, NC>), dim3(grid), dim3(64 * WAVES), 0, s, a, per_min)
+    if (m.d_h == 128) {
+        if (columns <= 16) CC_FEW(128, 1);
+        else if (columns <= 32) CC_FEW(128, 2);
+        else CC_FEW(128, 4);
+    } else {
+        if (columns <= 16) CC_FEW(64, 1);
+        else if (columns <= 32) CC_FEW(64, 2);
+        else CC_FEW(64, 4);
+    }
+#undef CC_FEW
 }

@@ -9,8 +9,11 @@
 
 #include "cacheclip.h"
 
-#define CC_PAGED_MAX_N 2048        // sequences of a batch of new rows
+#define CC_PAGED_MAX_N 1024        // sequences of a batch of new rows
 #define CC_PAGED_MAX_COLUMNS (1 << 20)   // (row, query head of a group) columns of one call
+#define CC_PAGED_WGS 256           // most workgroups of an attention launch that leave pieces, two slots each
+#define CC_PAGED_SLOT (64 * (128 + 4))   // floats of the largest piece
+#define CC_PAGED_CTX_INTS (CC_PAGED_WGS + 64)   // of a context: a count per workgroup, and 128 bf16 zeros
 #define CC_PAGE_LAYERS 128         // layers whose pages one copy launch takes (their addresses are kernel arguments)
 
 // Scratch of a pool, in ints: a header, per sequence (marks, takes, offsets), per page (two lists, a map), and the copies
@@ -27,7 +30,7 @@ inline cc_page_work cc_page_work_layout(int64_t n_pages, int64_t n_seqs) {
     const int64_t n = std::max(n_pages, n_seqs);
     w.src = take(n), w.dst = take(n), w.rows = take(n);
     w.attn = at;
-    w.ints = at;
+    w.ints = at + (int64_t)2 * CC_PAGED_WGS * CC_PAGED_SLOT;
     return w;
 }
 
@@ -98,7 +101,7 @@ inline cc_refusal cc_check_list(int32_t n, int32_t n_seqs, const int32_t* a, con
 
 inline cc_refusal cc_check_new_rows(const cc_new_rows* r, int32_t n_seqs, int32_t g) {
     CC_REFUSE_IF(!r, CC_ERR_NULL, "rows must not be NULL");
-    CC_REFUSE_IF(r->n < 0 || r->n > CC_PAGED_MAX_N, CC_ERR_SHAPE, "n must be in [0, 2048]");
+    CC_REFUSE_IF(r->n < 0 || r->n > CC_PAGED_MAX_N, CC_ERR_SHAPE, "n must be in [0, 1024]");
     CC_REFUSE_IF(r->rows < 0 || r->max_new < 0 || (int64_t)r->rows * g > CC_PAGED_MAX_COLUMNS, CC_ERR_SHAPE,
                  "need rows >= 0, max_new >= 0 and at most 2^20 rows times query heads of a group");
     CC_REFUSE_IF(r->n > 0 && !r->start, CC_ERR_NULL, "start must not be NULL");

@@ -116,9 +116,9 @@ def test_list_and_row_checks(lib):
         f.update(kw)
         return lib.new_rows(C.byref(_NewRows(**f)), n_seqs, g)
 
-    assert rows() == rows(seq=None) == rows(n=0, start=None) == rows(n=2048) == rows(rows=0) == rows(rows=1 << 18) == CC_OK
+    assert rows() == rows(seq=None) == rows(n=0, start=None) == rows(n=1024) == rows(rows=0) == rows(rows=1 << 18) == CC_OK
     assert lib.new_rows(None, 4, 1) == rows(start=None) == CC_ERR_NULL
-    for bad in (dict(n=-1), dict(n=2049), dict(rows=-1), dict(max_new=-1), dict(rows=(1 << 18) + 1), dict(seq=None, n_seqs=2),
+    for bad in (dict(n=-1), dict(n=1025), dict(rows=-1), dict(max_new=-1), dict(rows=(1 << 18) + 1), dict(seq=None, n_seqs=2),
                 dict(start=A + 2), dict(seq=A + 1)):
         assert rows(**bad) == CC_ERR_SHAPE, bad
 
