@@ -36,7 +36,7 @@ template <int OFF>
 __device__ __forceinline__ void dma16(const char* gsrc_minus_off, char* lds_wave_base) {
     static_assert(OFF >= 0 && OFF < 4096, "the instruction offset is 13 bits signed");
     __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)gsrc_minus_off,
-                                     (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 0);
+                                     (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 2);   // non-temporal: read once
 }
 // LDS reads by hand: the compiler would wait for all loads into LDS before each.  Every read is issued and waited for in one
 // basic block.
@@ -63,6 +63,21 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t uniform(int64_t v) {
     return ((int64_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
+}
+
+__device__ __forceinline__ const char* scalar_ptr(const char* p) {
+    return (const char*)uniform((int64_t)(uintptr_t)p);
+}
+
+// Pieces of cut blocks go from one XCD to another: eight bytes written past the L2 and read past it.  A fence over the whole
+// L2 instead (every workgroup's write-back and invalidation, 32 workgroups an L2) cost 70 to 110 us a call.
+__device__ __forceinline__ void put(float* p, float x, float y) {
+    const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get(const float* p) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
 // Key tiles of `keys` keys that the rows of a sequence see: the first `sink` tiles, then those from `from` to the end.
@@ -178,14 +193,14 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
     auto kswz = [](int r) { return D_H == 128 ? (r & 15) : ((r >> 1) & 7); };
     auto vswz = [](int r) { return D_H == 128 ? (r & 7) : ((r >> 1) & 3); };
     const int l_row = lane / CPR, l_c = lane % CPR;
-    uint32_t k_col[HL], v_col[HL];                        // byte within the row that load i of 16 keys fetches
+    const uint32_t st_b = (uint32_t)a.st_tok * 2;
+    uint32_t k_off[HL], v_off[HL];                        // from the first of 16 rows, of the lane's 16 bytes of load i
 #pragma unroll
     for (int i = 0; i < HL; ++i) {
         const int r = i * RPI + l_row;
-        k_col[i] = (l_c ^ kswz(r)) * 16;
-        v_col[i] = (l_c ^ (2 * vswz(r))) * 16;
+        k_off[i] = r * st_b + (l_c ^ kswz(r)) * 16;
+        v_off[i] = r * st_b + (l_c ^ (2 * vswz(r))) * 16;
     }
-    const uint32_t st_b = (uint32_t)a.st_tok * 2;
     char* const my_ring = ring[w];
     const uint32_t ring_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)my_ring;
     uint32_t kaddr[KS];
@@ -265,47 +280,58 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         const __attribute__((address_space(4))) int32_t* row_table =
             (const __attribute__((address_space(4))) int32_t*)(a.p.table + s * a.p.st_table);
         const int64_t head_off = (int64_t)h * a.st_head;
-        // 16 keys from key0 on, in one page: its first row in K or V, or zeros for what no page holds
-        struct half_src { const char* k; const char* v; int rmax; };
-        auto half_of = [&](int key0) -> half_src {
-            half_src r;
-            const int page = key0 < L ? row_table[key0 >> a.p.shift] : -1;
-            if ((unsigned)page < (unsigned)a.p.n_pages) {
-                const int64_t at = (page * a.st_page + (int64_t)(key0 & ((1 << a.p.shift) - 1)) * a.st_tok + head_off) * 2;
-                r.k = (const char*)a.K + at;
-                r.v = (const char*)a.V + at;
-                r.rmax = min(15, L - 1 - key0);            // rows behind the last token repeat it (they are masked)
+        // The two pages of a tile (16 keys each, in one page), asked for a tile ahead of the loads that need them.
+        struct pages { int a, b; };
+        auto pages_of = [&](int k) __attribute__((always_inline)) -> pages {
+            const int key0 = tile_key(k), end = max(L - 1, 0);
+            return {row_table[min(key0, end) >> a.p.shift], row_table[min(key0 + 16, end) >> a.p.shift]};
+        };
+        // First row of 16 keys as an offset into K and V, and its last one: rows behind the last token repeat it (they are
+        // masked); rmax < 0: zeros, for what no page holds.
+        struct rows16 { int64_t at; int rmax; };
+        auto rows_of = [&](int key0, int page) __attribute__((always_inline)) -> rows16 {
+            const bool there = key0 < L && (unsigned)page < (unsigned)a.p.n_pages;
+            return {(page * a.st_page + (int64_t)(key0 & ((1 << a.p.shift) - 1)) * a.st_tok + head_off) * 2,
+                    there ? min(15, L - 1 - key0) : -1};
+        };
+        // (a scalar base and a 32-bit lane offset: 64-bit vector addresses cost more to make than the loads to issue)
+        auto load = [&](const bf16_t* base, rows16 r, const uint32_t* off16, char* dst) __attribute__((always_inline)) {
+            const char* src = (const char*)base + r.at;
+            if (r.rmax == 15) {
+                static_for<HL>([&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value;
+                    uint32_t off = off16[i];
+                    asm volatile("" : "+v"(off));
+                    dma16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
+                });
             } else {
-                r.k = r.v = (const char*)a.zeros;
-                r.rmax = 0;
+                if (r.rmax < 0) src = (const char*)a.zeros;
+                static_for<HL>([&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value;
+                    const int row = i * RPI + l_row;
+                    uint32_t off = off16[i] - (uint32_t)(row - min(row, max(r.rmax, 0))) * st_b;
+                    asm volatile("" : "+v"(off));
+                    dma16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
+                });
             }
-            return r;
         };
-        auto load = [&](const char* src, int rmax, const uint32_t* col, char* dst) __attribute__((always_inline)) {
-            static_for<HL>([&](auto ic) __attribute__((always_inline)) {
-                constexpr int i = decltype(ic)::value;
-                const uint32_t off = (uint32_t)min(i * RPI + l_row, rmax) * st_b + col[i];
-                dma16<i * 1024>(src - i * 1024 + off, dst);
-            });
-        };
-        auto load_k = [&](int k) __attribute__((always_inline)) {
-            const int key0 = tile_key(k);
-            char* dst = my_ring + (k % NS) * 2 * TILE;
-            const half_src x = half_of(key0), y = half_of(key0 + 16);
-            load(x.k, x.rmax, k_col, dst);
-            load(y.k, y.rmax, k_col, dst + TILE / 2);
-        };
-        auto load_v = [&](int k) __attribute__((always_inline)) {
-            const int key0 = tile_key(k);
-            char* dst = my_ring + (k % NS) * 2 * TILE + TILE;
-            const half_src x = half_of(key0), y = half_of(key0 + 16);
-            load(x.v, x.rmax, v_col, dst);
-            load(y.v, y.rmax, v_col, dst + TILE / 2);
-        };
-        for (int k = 0; k < NS && k < nt; ++k) {
-            load_k(k);
-            load_v(k);
+        auto stage_of = [&](int k) { return my_ring + (k % NS) * 2 * TILE; };
+        {
+            pages pg[NS];
+#pragma unroll
+            for (int k = 0; k < NS; ++k) pg[k] = pages_of(min(k, max(nt - 1, 0)));
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+                if (k < nt) {
+                    const int key0 = tile_key(k);
+                    const rows16 x = rows_of(key0, pg[k].a), y = rows_of(key0 + 16, pg[k].b);
+                    load(a.K, x, k_off, stage_of(k));
+                    load(a.K, y, k_off, stage_of(k) + TILE / 2);
+                    load(a.V, x, v_off, stage_of(k) + TILE);
+                    load(a.V, y, v_off, stage_of(k) + TILE + TILE / 2);
+                }
         }
+        pages pg_next = pages_of(max(0, min(NS, nt - 1)));
         // Loads younger than K(k): V(k) and the pairs of up to NS - 1 later tiles; than V(k): those and K(k + NS).
         auto wait_k = [&](int rem) __attribute__((always_inline)) {
             static_for<NS>([&](auto jc) __attribute__((always_inline)) {
@@ -337,7 +363,11 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                              :: "memory");
             else
                 asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1])::"memory");
-            if (rem >= NS) load_k(k + NS);
+            const rows16 x = rows_of(tile_key(k + NS), pg_next.a), y = rows_of(tile_key(k + NS) + 16, pg_next.b);
+            if (rem >= NS) {
+                load(a.K, x, k_off, stage_of(k));
+                load(a.K, y, k_off, stage_of(k) + TILE / 2);
+            }
             f32x4 sc[NC][2];
 #pragma unroll
             for (int nc = 0; nc < NC; ++nc) {
@@ -415,7 +445,11 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                          :: "memory");
             if constexpr (DT == 8)
                 asm volatile("" : "+v"(va[4]), "+v"(vb[4]), "+v"(va[5]), "+v"(vb[5]), "+v"(va[6]), "+v"(vb[6]), "+v"(va[7]), "+v"(vb[7])::"memory");
-            if (rem >= NS) load_v(k + NS);
+            if (rem >= NS) {
+                load(a.V, x, v_off, stage_of(k) + TILE);
+                load(a.V, y, v_off, stage_of(k) + TILE + TILE / 2);
+            }
+            pg_next = pages_of(min(k + 1 + NS, nt - 1));
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const bf16x8 vf = __builtin_shufflevector(va[dt], vb[dt], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -464,7 +498,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                 for (int j = 0; j < WAVES; ++j)
                     r += x[j].x * *reinterpret_cast<const f32x4*>(ring[j] + ((dt * NC + nc) * 64 + lane) * 16);
                 if (!whole) {
-                    *reinterpret_cast<f32x4*>(piece + ((dt * NC + nc) * 64 + lane) * 4) = r;
+                    put(piece + ((dt * NC + nc) * 128 + lane) * 2, r[0], r[1]);
+                    put(piece + ((dt * NC + nc) * 128 + 64 + lane) * 2, r[2], r[3]);
                 } else if (i < n_new) {
                     bf16x4 out;
 #pragma unroll
@@ -472,7 +507,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                     *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * kg) = out;
                 }
             }
-            if (!whole && w == 0 && kg == 0) *reinterpret_cast<float2*>(piece + COLS * D_H + (nc * 16 + c16) * 2) = make_float2(m, l);
+            if (!whole && w == 0 && kg == 0) put(piece + COLS * D_H + (nc * 16 + c16) * 2, m, l);
         }
         if (whole) {
             __syncthreads();                               // the rings are free again
@@ -480,16 +515,15 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         }
         // ---- a cut block: the workgroup that comes last adds the pieces, in the order of their keys ----
         const int w0 = (int)((u0 + START) / per), w1 = (int)((u1 - 1) / per);
-        __threadfence();
+        wait_loads<0>();                                   // the piece is written
         __syncthreads();
         if (tid == 0) {
-            const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+            const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             last_here = before == w1 - w0;
             if (last_here) __hip_atomic_store(&a.arrived[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         __syncthreads();
         if (!last_here) continue;
-        __threadfence();
         for (int e = tid; e < DT * NC * 64; e += 64 * WAVES) {
             const int ln = e & 63, dn = e >> 6, nc = dn % NC, dt = dn / NC;
             const int cc = nc * 16 + (ln & 15), col = blk * COLS + cc, i = col / a.g, hg = col - i * a.g;
@@ -498,8 +532,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             f32x4 r = {0.f, 0.f, 0.f, 0.f};
             for (int j = w0; j <= w1; ++j) {
                 const float* pc = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * COLS * (D_H + 2);
-                const float2 x = *reinterpret_cast<const float2*>(pc + COLS * D_H + cc * 2);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(pc + e * 4);
+                const float2 x = get(pc + COLS * D_H + cc * 2), va = get(pc + (dn * 128 + ln) * 2), vb = get(pc + (dn * 128 + 64 + ln) * 2);
+                const f32x4 v = {va.x, va.y, vb.x, vb.y};
                 const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.0f : mn;
                 const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(x.x - ref);
                 l = l * keep + x.y * f;
