@@ -717,7 +717,7 @@ cc_status cc_step_paged_attention(cc_ctx* c, const void* q, const cc_new_rows* r
     CC_REFUSE(c, cc_check_paged_kv(kv, pool->page_size, c->m.H_kv, c->m.d_h));
     CC_REFUSE(c, cc_check_new_rows(rows, pool->n_seqs, c->m.H_q / c->m.H_kv));
     if (rows->rows > 0 && (!q || !o)) return fail(c, CC_ERR_NULL, "q and o must not be NULL");
-    if (window < 0 || sinks < 0) return fail(c, CC_ERR_SHAPE, "window and sinks must be >= 0");
+    CC_REFUSE(c, cc_check_attend(*rows, *pool, c->m.H_q / c->m.H_kv, window, sinks));
     if (!aligned16(q) || !aligned16(o)) return fail(c, CC_ERR_SHAPE, "buffers must be 16-byte aligned");
     device_scope dev(c->device);
     if (flags & CC_FLAG_CHECK_IDX) {

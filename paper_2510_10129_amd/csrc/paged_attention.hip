@@ -13,9 +13,11 @@
 // column, its scores are laid out as the second product's operand needs them, and the rescale factor is one number per
 // lane.  The running maximum moves only when a score exceeds it by more than 2^8 (in base 2), so most tiles need neither an
 // exchange between lanes nor a rescale; probabilities up to 2^8 in bf16 and sums in fp32 cancel in the final division.
+//
+// Many rows (chunk_attn_kernel): the loop of the contiguous cache's attention (attend.h), 256 columns a workgroup, with the
+// key tiles of all (sequence, row tile, kv head) blocks in equal ranges, and pieces put together as above.
+#include "attend.h"
 #include "paged.h"
-
-#include <type_traits>
 
 namespace {
 
@@ -23,75 +25,22 @@ constexpr int KEYS = 32;                      // of a tile of few_attn_kernel
 constexpr int WAVES = 4;
 constexpr int START = 4;                      // units that a block costs besides its tiles: its queries, first loads and result
 
-template <int NI, int I = 0, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-    if constexpr (I < NI) {
-        f(std::integral_constant<int, I>{});
-        static_for<NI, I + 1>(f);
-    }
-}
-
 // 16 bytes per lane from global memory into LDS at wave base + OFF + 16 * lane; OFF is added to the global address too.
+// Non-temporal: what few rows read is read once.
 template <int OFF>
-__device__ __forceinline__ void dma16(const char* gsrc_minus_off, char* lds_wave_base) {
+__device__ __forceinline__ void stream16(const char* gsrc_minus_off, char* lds_wave_base) {
     static_assert(OFF >= 0 && OFF < 4096, "the instruction offset is 13 bits signed");
     __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)gsrc_minus_off,
-                                     (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 2);   // non-temporal: read once
+                                     (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 2);
 }
-// LDS reads by hand: the compiler would wait for all loads into LDS before each.  Every read is issued and waited for in one
-// basic block.
-template <int IMM>
-__device__ __forceinline__ bf16x8 lds_read_b128(uint32_t addr) {
-    bf16x8 v;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(IMM));
-    return v;
-}
-// Transposing read: within 16 lanes, lane i receives as element e element i % 4 of the 8 bytes addressed by lane i / 4 + 4 e.
-template <int IMM>
-__device__ __forceinline__ bf16x4 lds_read_tr(uint32_t addr) {
-    bf16x4 v;
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(IMM));
-    return v;
-}
-// At most N of this wave's loads from memory still on their way.
+// At most N of this wave's loads and stores still on their way.
 template <int N>
 __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
     asm volatile("" ::: "memory");
 }
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-    return ((int64_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
-}
-
 __device__ __forceinline__ const char* scalar_ptr(const char* p) {
     return (const char*)uniform((int64_t)(uintptr_t)p);
-}
-
-// Pieces of cut blocks go from one XCD to another: eight bytes written past the L2 and read past it.  A fence over the whole
-// L2 instead (every workgroup's write-back and invalidation, 32 workgroups an L2) cost 70 to 110 us a call.
-__device__ __forceinline__ void put(float* p, float x, float y) {
-    const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get(const float* p) {
-    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
-// Key tiles of `keys` keys that the rows of a sequence see: the first `sink` tiles, then those from `from` to the end.
-struct tile_span {
-    int sink, from, count;
-    __device__ __forceinline__ int tile(int t) const { return t < sink ? t : t - sink + from; }
-};
-__device__ __forceinline__ tile_span visible_tiles(int first, int L, int window, int sinks, int keys) {
-    tile_span s;
-    const int low = window > 0 ? (int)max((int64_t)0, (int64_t)first - window + 1) : 0;
-    s.from = low / keys;
-    s.sink = window > 0 ? min((int)(((int64_t)sinks + keys - 1) / keys), s.from) : 0;
-    s.count = max(1, s.sink + (L + keys - 1) / keys - s.from);       // a row that sees nothing still has its zeros to write
-    return s;
 }
 
 struct paged_args {
@@ -276,9 +225,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         // ---- loads of the wave's k-th tile ----
         const int nt = te - ta > w ? (te - ta - w + WAVES - 1) / WAVES : 0;
         auto tile_key = [&](int k) { return span.tile(ta + w + k * WAVES) * KEYS; };
-        // (constant for the launch: scalar loads, which do not count among the loads that the waits below count)
-        const __attribute__((address_space(4))) int32_t* row_table =
-            (const __attribute__((address_space(4))) int32_t*)(a.p.table + s * a.p.st_table);
+        // (scalar loads do not count among the loads that the waits below count)
+        const in_pages::table_t row_table = (in_pages::table_t)(a.p.table + s * a.p.st_table);
         const int64_t head_off = (int64_t)h * a.st_head;
         // The two pages of a tile (16 keys each, in one page), asked for a tile ahead of the loads that need them.
         struct pages { int a, b; };
@@ -302,7 +250,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                     constexpr int i = decltype(ic)::value;
                     uint32_t off = off16[i];
                     asm volatile("" : "+v"(off));
-                    dma16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
+                    stream16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
                 });
             } else {
                 if (r.rmax < 0) src = (const char*)a.zeros;
@@ -311,7 +259,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                     const int row = i * RPI + l_row;
                     uint32_t off = off16[i] - (uint32_t)(row - min(row, max(r.rmax, 0))) * st_b;
                     asm volatile("" : "+v"(off));
-                    dma16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
+                    stream16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
                 });
             }
         };
@@ -354,8 +302,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             bf16x8 kf[2][KS];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                kf[0][ks] = lds_read_b128<0>(kaddr[ks] + stage);
-                kf[1][ks] = lds_read_b128<16 * ROW>(kaddr[ks] + stage);
+                kf[0][ks] = lds_read_b128_at<0>(kaddr[ks] + stage);
+                kf[1][ks] = lds_read_b128_at<16 * ROW>(kaddr[ks] + stage);
             }
             if constexpr (KS == 4)
                 asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1]), "+v"(kf[0][2]),
@@ -374,10 +322,10 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                 if constexpr (Q_LDS) {
                     static_assert(!Q_LDS || KS == 4, "four fragments a column block");
                     const uint32_t at = q_at + nc * KS * 1024;
-                    qf[0][0] = lds_read_b128<0>(at);
-                    qf[0][1] = lds_read_b128<1024>(at);
-                    qf[0][KS - 2] = lds_read_b128<(KS - 2) * 1024>(at);
-                    qf[0][KS - 1] = lds_read_b128<(KS - 1) * 1024>(at);
+                    qf[0][0] = lds_read_b128_at<0>(at);
+                    qf[0][1] = lds_read_b128_at<1024>(at);
+                    qf[0][KS - 2] = lds_read_b128_at<(KS - 2) * 1024>(at);
+                    qf[0][KS - 1] = lds_read_b128_at<(KS - 1) * 1024>(at);
                     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(qf[0][0]), "+v"(qf[0][1]), "+v"(qf[0][KS - 2]), "+v"(qf[0][KS - 1]));
                 }
 #pragma unroll
@@ -437,8 +385,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             bf16x4 va[DT], vb[DT];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-                va[dt] = lds_read_tr<0>(vaddr[dt] + stage);
-                vb[dt] = lds_read_tr<16 * ROW>(vaddr[dt] + stage);
+                va[dt] = lds_read_tr_at<0>(vaddr[dt] + stage);
+                vb[dt] = lds_read_tr_at<16 * ROW>(vaddr[dt] + stage);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(vb[0]), "+v"(va[1]), "+v"(vb[1]), "+v"(va[2]), "+v"(vb[2]),
                          "+v"(va[3]), "+v"(vb[3])
@@ -549,6 +497,155 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
     }
 }
 
+constexpr int CHUNK_START = 5;                // units of a block besides its key tiles, as in the even grids of attention.hip
+constexpr int MAX_BLOCKS = CC_PAGED_MAX_COLUMNS / 256 + CC_PAGED_MAX_N;
+
+// A workgroup of eight waves per range.  Blocks are numbered e0(b) + row tile with e0(b) = floor(columns in front of b / 256) + b:
+// at least as many numbers as sequence b has row tiles, the unused ones of length 0, and no scan is needed to find one.
+template <int D_H>
+__global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int per_min) {
+    __shared__ __align__(16) bf16_t smem[LDS_TILES * BN_KEYS * D_H];
+    __shared__ int simd_waves[4], group_waves[2], wave_units[8], last_here;
+    __shared__ int pre[MAX_BLOCKS + 1];
+    __shared__ int e0[CC_PAGED_MAX_N + 1], rows_of[CC_PAGED_MAX_N], len_of[CC_PAGED_MAX_N];
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+    int grp, widx;
+    wave_role(simd_waves, group_waves, grp, widx);
+
+    auto sequence_of = [&](int e) -> int {                // the last one with e0 <= e
+        int b = 0;
+        for (int hi = a.n - 1; b < hi;) {
+            const int mid = (b + hi + 1) >> 1;
+            if (e0[mid] <= e) b = mid; else hi = mid - 1;
+        }
+        return b;
+    };
+    // ---- units in front of every block of a head ----
+    {
+        const int base = max(0, min(a.start[0], a.rows));
+        for (int b = tid; b <= a.n; b += 512) {
+            const int r = max(base, min(a.start[b], a.rows));
+            e0[b] = (int)((int64_t)(r - base) * a.g / 256) + b;
+            if (b < a.n) {
+                const batch_seq s = seq_of(a, b);
+                rows_of[b] = s.n;
+                len_of[b] = s.L;
+            }
+        }
+        __syncthreads();
+        const int blocks = min(e0[a.n], MAX_BLOCKS);
+        int carry = 0;
+        for (int i0 = 0; i0 < blocks; i0 += 512) {
+            const int e = i0 + tid;
+            int len = 0;
+            if (e < blocks) {
+                const int b = sequence_of(e);
+                const int c0 = (e - e0[b]) * 256, n = rows_of[b], first = len_of[b] - n;
+                if (c0 >= 0 && c0 < n * a.g) {
+                    const int end = first + min(n - 1, (c0 + 255) / a.g) + 1;
+                    len = visible_tiles(first + c0 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS).count + CHUNK_START;
+                }
+            }
+            int inc = len;
+            for (int off = 1; off < 64; off <<= 1) {
+                const int v = __shfl_up(inc, off);
+                if (lane >= off) inc += v;
+            }
+            if (lane == 63) wave_units[w] = inc;
+            __syncthreads();
+            int before = carry;
+            for (int j = 0; j < 8; ++j) {
+                if (j < w) before += wave_units[j];
+                carry += wave_units[j];
+            }
+            if (e < blocks) pre[e] = before + inc - len;
+            __syncthreads();
+        }
+        if (tid == 0) pre[blocks] = carry;
+        __syncthreads();
+    }
+    const int blocks = uniform(min(e0[a.n], MAX_BLOCKS)), head_units = uniform(pre[blocks]);
+    const int64_t total = (int64_t)head_units * a.H_kv;
+    const int n_wg = gridDim.x;
+    const int64_t per = max((int64_t)per_min, (total + n_wg - 1) / n_wg);
+    // workgroup ids go round-robin to the 8 XCDs: each gets consecutive ranges
+    const int x = blockIdx.x & 7, xq = n_wg >> 3, xr = n_wg & 7;
+    const int range = x * xq + min(x, xr) + (int)(blockIdx.x >> 3);
+    int64_t u = range * per;
+    const int64_t stop = min(u + per, total);
+    while (u < stop) {
+        const int kvh = (int)(u / head_units), uh = (int)(u - (int64_t)kvh * head_units);
+        int e = 0;
+        for (int i = lane; i - lane < blocks; i += 64) e += __popcll(__ballot(i < blocks && pre[min(i, blocks - 1) + 1] <= uh));
+        e = uniform(e);
+        const int b = uniform(sequence_of(e));
+        const int b0 = uniform(pre[e]), len = uniform(pre[e + 1]) - b0, rt = e - uniform(e0[b]);
+        const batch_seq sq = seq_of(a, b);
+        const int n_new = uniform(sq.n), L = uniform(sq.L), first = L - n_new;
+        const int ta = max(0, uh - b0 - CHUNK_START), te = (int)min((int64_t)len, uh - b0 + (stop - u)) - CHUNK_START;
+        const int64_t u0 = (int64_t)kvh * head_units + b0;
+        u = u0 + len;
+        if (te <= ta) continue;
+        in_pages keys;
+        keys.table = (in_pages::table_t)(a.p.table + uniform(sq.s) * a.p.st_table);
+        keys.K = a.K, keys.V = a.V, keys.zeros = a.zeros;
+        keys.st_page = a.st_page, keys.st_tok = a.st_tok, keys.sh = a.st_head;
+        keys.shift = a.p.shift, keys.n_pages = a.p.n_pages, keys.L = L, keys.first = first, keys.row0 = uniform(sq.row0);
+        keys.window = a.window, keys.sinks = a.sinks;
+        const int end = first + min(n_new - 1, (rt * 256 + 255) / a.g) + 1;
+        keys.span = visible_tiles(first + rt * 256 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS);
+        const bool whole = ta == 0 && te == keys.span.count;
+        const int w0 = (int)((u0 + CHUNK_START) / per), w1 = (int)((u0 + len - 1) / per);
+        attend<D_H, true, uint32_t>(keys, a.q, n_new, a.H_q, a.g, a.o, a.scale_log2, a.part, smem, grp, widx, kvh, rt, ta, te - ta,
+                                    whole ? -1 : 2 * range + (w0 == range ? 1 : 0));
+        if (whole) continue;
+        // ---- a cut block: the workgroup that comes last adds the pieces, in the order of their keys ----
+        wait_loads<0>();                                   // the piece is written
+        __syncthreads();
+        if (tid == 0) {
+            const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last_here = before == w1 - w0;
+            if (last_here) __hip_atomic_store(&a.arrived[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last_here) continue;
+        // a thread holds what the lane that left it did: half of a column's sums
+        constexpr int NG = D_H / 8;
+        const int col = rt * 256 + w * 32 + (lane & 31), mi = col / a.g, hg = col - mi * a.g;
+        if (mi < n_new) {
+            f32x4 acc[NG];
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = w0; j <= w1; ++j) {
+                const float* pp = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * 256 * (D_H + 4) + w * 32 * (D_H + 4);
+                const float2 ml = get(pp + 32 * D_H + lane * 2);
+                float2 v[NG][2];
+#pragma unroll
+                for (int k = 0; k < NG; ++k) {
+                    v[k][0] = get(pp + k * 256 + lane * 2);
+                    v[k][1] = get(pp + k * 256 + 128 + lane * 2);
+                }
+                const float mn = fmaxf(m, ml.x), ref = mn == -INFINITY ? 0.0f : mn;
+                const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+                l = l * keep + ml.y * f;
+                m = mn;
+#pragma unroll
+                for (int k = 0; k < NG; ++k) acc[k] = acc[k] * keep + f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y} * f;
+            }
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            bf16_t* op = a.o + ((int64_t)(keys.row0 + mi) * a.H_q + kvh * a.g + hg) * D_H + 4 * (lane >> 5);
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                bf16x4 r;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[i] = (bf16_t)(acc[k][i] * inv);
+                *reinterpret_cast<bf16x4*>(op + 8 * k) = r;
+            }
+        }
+    }
+}
+
 }  // namespace
 
 void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_page_pool& p, const cc_paged_kv& kv, int window,
@@ -562,6 +659,12 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
     const int grid = std::min(cc_device_cus(), CC_PAGED_WGS);
     const int64_t columns = (int64_t)std::min(r.max_new, r.rows) * g;
     const int per_min = 2 * WAVES + START;
+    if (columns > 64) {
+        const int chunk_min = 3 + CHUNK_START;
+        if (m.d_h == 128) hipLaunchKernelGGL(chunk_attn_kernel<128>, dim3(grid), dim3(512), 0, s, a, chunk_min);
+        else hipLaunchKernelGGL(chunk_attn_kernel<64>, dim3(grid), dim3(512), 0, s, a, chunk_min);
+        return;
+    }
 #define CC_FEW(D, NC) hipLaunchKernelGGL((few_attn_kernel<D, NC>), dim3(grid), dim3(64 * WAVES), 0, s, a, per_min)
     if (m.d_h == 128) {
         if (columns <= 16) CC_FEW(128, 1);

@@ -12,7 +12,7 @@
 #define CC_PAGED_MAX_N 1024        // sequences of a batch of new rows
 #define CC_PAGED_MAX_COLUMNS (1 << 20)   // (row, query head of a group) columns of one call
 #define CC_PAGED_WGS 256           // most workgroups of an attention launch that leave pieces, two slots each
-#define CC_PAGED_SLOT (64 * (128 + 4))   // floats of the largest piece
+#define CC_PAGED_SLOT (256 * (128 + 4))  // floats of the largest piece
 #define CC_PAGED_CTX_INTS (CC_PAGED_WGS + 64)   // of a context: a count per workgroup, and 128 bf16 zeros
 #define CC_PAGE_LAYERS 128         // layers whose pages one copy launch takes (their addresses are kernel arguments)
 
@@ -107,6 +107,14 @@ inline cc_refusal cc_check_new_rows(const cc_new_rows* r, int32_t n_seqs, int32_
     CC_REFUSE_IF(r->n > 0 && !r->start, CC_ERR_NULL, "start must not be NULL");
     CC_REFUSE_IF(!r->seq && r->n > n_seqs, CC_ERR_SHAPE, "without seq, n must be at most n_seqs");
     CC_REFUSE_IF(!cc_aligned(r->start, 4) || !cc_aligned(r->seq, 4), CC_ERR_SHAPE, "start and seq must be 4-byte aligned");
+    return {CC_OK, ""};
+}
+
+// Key tiles that the blocks of a head can add up to are counted in 32 bits.
+inline cc_refusal cc_check_attend(const cc_new_rows& r, const cc_page_pool& p, int32_t g, int32_t window, int32_t sinks) {
+    CC_REFUSE_IF(window < 0 || sinks < 0, CC_ERR_SHAPE, "window and sinks must be >= 0");
+    const int64_t blocks = (int64_t)r.rows * g / 256 + r.n, tiles = ((int64_t)p.max_pages * p.page_size + 63) / 64 + 8;
+    CC_REFUSE_IF(blocks * tiles >= (1ll << 31), CC_ERR_SHAPE, "rows of the batch times columns of the table are too many for one call");
     return {CC_OK, ""};
 }
 
