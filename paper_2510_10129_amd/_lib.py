@@ -186,24 +186,47 @@ class KVLayer:
 
 def _i32(t, what: str, dims: int = 1):
     """A device list as the library reads it: int32, unit stride."""
-    if t.dtype != _torch().int32 or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if t.dtype is not _torch.int32 or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{what} must be an int32 tensor of {dims} dimension(s) with unit stride")
     return t
 
 
 def _bf16(t, what: str):
-    if t.dtype != _torch().bfloat16:
+    if t.dtype is not _torch.bfloat16:
         raise ValueError(f"{what} must be a bfloat16 tensor")
     return t
 
 
-def _torch():
-    import torch
-    return torch
+class _Module:
+    """torch, imported when first asked for something."""
+
+    def __getattr__(self, name):
+        import torch
+        global _torch
+        _torch = torch
+        return getattr(torch, name)
+
+
+_torch = _Module()
+
+
+class _Described:
+    """What a call is told of a pool, a layer's pages, a batch or a rotary rule: checked and laid out for the library when first
+    used, and again after a field was assigned (the tensors themselves are described as they were then: what changes
+    their strides or their memory in place is not seen)."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_c", None)
+
+    def c_struct(self):
+        if self._c is None:
+            object.__setattr__(self, "_c", self._describe())
+        return self._c
 
 
 @dataclass
-class PagePool:
+class PagePool(_Described):
     """Pages that sequences hold by reference: refs [n_pages], table [n_seqs, max_pages], len [n_seqs] int32 on
     the device, page_size tokens a page.  status and work are allocated where they are not given.  `PagePool.empty`
     makes one with every page free."""
@@ -215,7 +238,7 @@ class PagePool:
     work: "object" = None
 
     def __post_init__(self):
-        torch = _torch()
+        torch = _torch
         _i32(self.refs, "refs"), _i32(self.table, "table", 2), _i32(self.len, "len")
         if self.table.shape[0] != self.len.shape[0]:
             raise ValueError("table and len must have a row for each sequence")
@@ -234,35 +257,42 @@ class PagePool:
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_seqs: int, max_pages: int, device="cuda"):
-        torch = _torch()
-        i32 = dict(dtype=torch.int32, device=device)
-        return cls(torch.zeros(n_pages, **i32), torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32), page_size)
+        i32 = dict(dtype=_torch.int32, device=device)
+        return cls(_torch.zeros(n_pages, **i32), _torch.full((n_seqs, max_pages), -1, **i32), _torch.zeros(n_seqs, **i32), page_size)
 
-    def c_struct(self) -> _Pool:
+    def _describe(self) -> _Pool:
         return _Pool(self.refs.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.status.data_ptr(),
                      self.work.data_ptr(), self.work.numel() * self.work.element_size(), self.table.stride(0),
                      self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1])
 
 
 @dataclass
-class PagedKV:
+class PagedKV(_Described):
     """One layer's pages: K, V torch bf16 tensors [n_pages, page_size, H_kv, d_h] (last dim contiguous; a view of
     [n_pages, H_kv, page_size, d_h] will do)."""
     K: "object"
     V: "object"
 
-    def c_struct(self, pool: PagePool, model) -> _PagedKV:
+    def _describe(self):
         K, V = _bf16(self.K, "K"), _bf16(self.V, "V")
-        shape = (pool.refs.numel(), pool.page_size, model.H_kv, model.d_h)
-        if K.shape != shape or V.shape != shape or K.stride() != V.stride() or K.stride(3) != 1:
-            raise ValueError(f"K and V must be {shape} with equal strides, the last of them 1")
-        if K.device != pool.refs.device or V.device != pool.refs.device:
-            raise ValueError("pages must lie on the pool's device")
-        return _PagedKV(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2))
+        if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.stride(3) != 1 or K.device != V.device:
+            raise ValueError("K and V must be of one shape, [n_pages, page_size, H_kv, d_h], with equal strides, the last of them 1")
+        return (K.data_ptr(), V.data_ptr()) + K.stride()[:3], tuple(K.shape), K.get_device()
+
+    @staticmethod
+    def table(kvs: Sequence["PagedKV"], pool: PagePool, model):
+        """The fields of a cc_paged_kv for each of kvs, one after the other, if the pages are those of the pool and the model."""
+        want, device, flat = (pool.c_struct().n_pages, pool.page_size, model.H_kv, model.d_h), pool.refs.get_device(), []
+        for kv in kvs:
+            fields, shape, lies_on = kv._c or kv.c_struct()
+            if shape != want or lies_on != device:
+                raise ValueError(f"K and V are {shape} on device {lies_on}; the pool and the model want {want} on {device}")
+            flat += fields
+        return flat
 
 
 @dataclass
-class NewRows:
+class NewRows(_Described):
     """New tokens of a batch: start int32 [n + 1] on the device, seq int32 [n] or None (sequence b is row b of the table),
     rows of the buffers, and a bound on the rows of one sequence."""
     start: "object"
@@ -270,7 +300,7 @@ class NewRows:
     rows: int
     max_new: int
 
-    def c_struct(self) -> _NewRows:
+    def _describe(self) -> _NewRows:
         n = _i32(self.start, "start").numel() - 1
         if n < 0 or (self.seq is not None and _i32(self.seq, "seq").numel() != n):
             raise ValueError("start must have one entry more than seq")
@@ -278,7 +308,7 @@ class NewRows:
 
 
 @dataclass
-class Rope:
+class Rope(_Described):
     """A rotary rule (cc_rope): scaling is "plain", "linear", "turns" or "index"."""
     base: float
     rot: int
@@ -290,7 +320,7 @@ class Rope:
     high: float = 4.0
     mscale: float = 1.0
 
-    def c_struct(self) -> _Rope:
+    def _describe(self) -> _Rope:
         if self.scaling not in ROPE_SCALINGS:
             raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
         return _Rope(self.base, self.rot, int(self.interleaved), ROPE_SCALINGS.index(self.scaling), self.orig_len, self.factor,
@@ -467,7 +497,8 @@ class Context:
 
     # ---- the paged cache of the answer phase ----
     def _layers(self, pool: PagePool, kvs: Sequence[PagedKV]):
-        return (_PagedKV * len(kvs))(*[kv.c_struct(pool, self.desc) for kv in kvs]), len(kvs)
+        n = len(kvs)                            # a _PagedKV is two addresses and three strides
+        return (_PagedKV * n).from_buffer(array("q", PagedKV.table(kvs, pool, self.desc))) if n else None, n
 
     def _pages(self, call, pool: PagePool, sync: bool, *args):
         p, host = pool.c_struct(), C.c_int32(0)
@@ -495,9 +526,10 @@ class Context:
         self._pages(self._lib.cc_compact_pages, pool, sync, *self._layers(pool, kvs))
 
     def _row_buffer(self, t, what: str, rows: int, width: int):
-        if _bf16(t, what).shape != (rows, width) or t.stride(1) != 1:
+        st = _bf16(t, what).stride()
+        if t.shape != (rows, width) or st[1] != 1:
             raise ValueError(f"{what} must be [{rows}, {width}] with unit column stride")
-        return t.stride(0) if rows > 1 else width
+        return st[0] if rows > 1 else width
 
     def step_rope_append(self, q, k, v, new: NewRows, pool: PagePool, kv: PagedKV, rope: Rope, q_out, pos=None, flags: int = 0):
         """q [rows, H_q*d_h], k, v [rows, H_kv*d_h] cuda bf16 (column slices of one product will do) -> q_out, pages of kv."""
@@ -508,7 +540,7 @@ class Context:
             raise ValueError("q_out must be contiguous")
         if pos is not None and _i32(pos, "pos").numel() < new.rows:
             raise ValueError("pos must have an entry for each row")
-        p, kvs, r, rule = pool.c_struct(), kv.c_struct(pool, m), new.c_struct(), rope.c_struct()
+        p, kvs, r, rule = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct(), rope.c_struct()
         self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st[0], k.data_ptr(), st[1], v.data_ptr(), st[2], C.byref(r),
                                                   _ptr(pos), C.byref(p), C.byref(kvs), C.byref(rule), q_out.data_ptr(), flags))
 
@@ -518,7 +550,7 @@ class Context:
         for t, what in ((q, "q"), (o, "o")):
             if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
                 raise ValueError(f"{what} must be contiguous")
-        p, kvs, r = pool.c_struct(), kv.c_struct(pool, m), new.c_struct()
+        p, kvs, r = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct()
         self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,
                                                       o.data_ptr(), flags))
 

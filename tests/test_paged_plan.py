@@ -162,12 +162,19 @@ def test_binding_refuses_what_the_library_cannot_read():
         cc.PagePool(torch.zeros(16, **i32)[::2], P.table, P.len, 16)
     m = _lib.ModelDesc(64, 4, 2, 64, 64, 1e4, 1e-5, 64, 64, 64)
     K = torch.zeros(8, 16, 2, 64, dtype=torch.bfloat16)
-    assert cc.PagedKV(K, K).c_struct(P, m).stride_page == 16 * 2 * 64
+    assert cc.PagedKV.table([cc.PagedKV(K, K)], P, m)[2:] == [16 * 2 * 64, 2 * 64, 64]
     by_head = torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16).transpose(1, 2)
-    assert cc.PagedKV(by_head, by_head).c_struct(P, m).stride_head == 16 * 64
+    assert cc.PagedKV.table([cc.PagedKV(by_head, by_head)], P, m)[2:] == [16 * 2 * 64, 64, 16 * 64]
     for bad in (K.float(), K[:4], K[..., :32], K.transpose(2, 3).contiguous().transpose(2, 3), by_head):
         with pytest.raises(ValueError):
-            cc.PagedKV(K, bad).c_struct(P, m)
+            cc.PagedKV.table([cc.PagedKV(K, bad)], P, m)
+    for other in (_torch_pool(n_pages=9), _torch_pool(page=32)):
+        with pytest.raises(ValueError):
+            cc.PagedKV.table([cc.PagedKV(K, K)], other, m)
+    kv = cc.PagedKV(K, K)
+    cc.PagedKV.table([kv], P, m)
+    kv.K = kv.V = by_head                                   # an assigned field is looked at again
+    assert cc.PagedKV.table([kv], P, m)[4] == 16 * 64
     start = torch.zeros(3, **i32)
     assert cc.NewRows(start, None, 4, 2).c_struct().n == 2
     for s, q in ((start, torch.zeros(3, **i32)), (start.float(), None), (start[:0], None), (torch.zeros(6, **i32)[::2], None)):
