@@ -298,20 +298,58 @@ struct rope_args {
     int32_t rot, interleaved;
     float mscale;
 };
-// A wave per row.  The row's (cos, sin) are computed once: the angle in turns in 64 bits (a far position's angle keeps
-// its fraction), its fraction's sine and cosine in 32.  A lane owns 16 bytes of a head and reads the pairs' other members
-// from where they lie; all loads of a head come before its stores, so queries may be turned in place.
-template <int D_H>
+enum { ROPE_HALVES = 0, ROPE_NEIGHBOURS = 1, ROPE_ODD_HALVES = 2 };
+// A wave per row and slice of its heads.  The row's (cos, sin) are computed once: the angle in turns in 64 bits (a far position's
+// angle keeps its fraction), its fraction's sine and cosine in 32.
+// A lane owns the same place of every head it comes to, so that its (cos, sin) stay in registers: where pairs lie half
+// of `rot` apart, 16 bytes of the low half and the 16 of the high half that belong to them (or 16 bytes that pass
+// through), so that a pair meets in one lane and queries may be turned in place; where they are neighbours, 16 bytes.  Halves that
+// are no multiple of 16 bytes take the pairs' other members one by one; a head is then read by one wave before it is written.
+// Up to four passes over heads are loaded before the first is stored, the first of them before the row's place is looked up: a
+// chain of start, length and page.  A chunk's rows are bound by HBM, a few rows by that chain.
+template <int D_H, int MODE>
 __global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf16_t* q, int64_t st_q, const bf16_t* __restrict__ k,
                                                           int64_t st_k, const bf16_t* __restrict__ v, int64_t st_v,
                                                           const int32_t* __restrict__ start, const int32_t* __restrict__ seq, int n,
                                                           int rows, const int32_t* __restrict__ pos, cc_pool_view p, bf16_t* Kp,
                                                           bf16_t* Vp, int64_t st_page, int64_t st_tok, int64_t st_head, int H_q,
-                                                          int H_kv, bf16_t* q_out) {
+                                                          int H_kv, bf16_t* q_out, int passes_per_slice) {
     constexpr int CPH = D_H / 8;
+    constexpr int NB = MODE == ROPE_ODD_HALVES ? 1 : 4;
     __shared__ float2 cs[4][64];
     const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int r = blockIdx.x * 4 + w;
+    const int r = blockIdx.x * 4 + w, row = min(r, rows - 1);
+    const int half = a.rot / 2, heads = H_q + 2 * H_kv;
+    const int units = MODE == ROPE_HALVES ? CPH - half / 8 : CPH;      // of a head
+    const int per_pass = 64 / units, my_head = lane / units, unit = lane - my_head * units;
+    const bool paired = MODE == ROPE_HALVES && unit < half / 8;
+    const int e0 = (MODE == ROPE_HALVES && !paired ? unit + half / 8 : unit) * 8;
+    const int h0 = (blockIdx.y * passes_per_slice) * per_pass + my_head;
+    const int h_end = min(heads, (int)(blockIdx.y + 1) * passes_per_slice * per_pass);
+    auto source = [&](int h) -> const bf16_t* {
+        const int hk = h - H_q, hv = hk - H_kv;
+        return hk < 0 ? q + row * st_q + h * D_H : hv < 0 ? k + row * st_k + hk * D_H : v + row * st_v + hv * D_H;
+    };
+    bf16x8 x[NB], y[NB];
+    auto load = [&](int hb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int h = hb + i * per_pass;
+            if (my_head >= per_pass || h >= h_end) continue;
+            const bf16_t* src = source(h) + e0;
+            x[i] = *reinterpret_cast<const bf16x8*>(src);
+            if (MODE == ROPE_HALVES && paired) y[i] = *reinterpret_cast<const bf16x8*>(src + half);
+            if (MODE == ROPE_ODD_HALVES && h < H_q + H_kv) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = e0 + e;
+                    y[i][e] = source(h)[j >= a.rot ? j : j < half ? j + half : j - half];
+                }
+            }
+        }
+    };
+    load(h0);
+
     const int b = r < rows ? cc_row_owner(start, n, r) : -1;
     int at = -1, page = -1;
     if (b >= 0) {
@@ -321,47 +359,59 @@ __global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf1
         if (at >= 0 && at < L) page = p.table[s * p.st_table + (at >> p.shift)];
         else at = -1;
     }
-    const int half = a.rot / 2;
     if (at >= 0 && lane < half) {
-        const double x = (double)(pos ? pos[r] : at) * a.turns[lane];
+        const double t = (double)(pos ? pos[r] : at) * a.turns[lane];
         float sn, c;
-        sincospif(2.0f * (float)(x - rint(x)), &sn, &c);
+        sincospif(2.0f * (float)(t - rint(t)), &sn, &c);
         cs[w][lane] = make_float2(c * a.mscale, sn * a.mscale);
     }
     __syncthreads();
-    if (at < 0) return;
+    if (at < 0 || my_head >= per_pass) return;
     const bool stored = (unsigned)page < (unsigned)p.n_pages;
     const int64_t slot = stored ? page * st_page + (int64_t)(at & ((1 << p.shift) - 1)) * st_tok : 0;
-    for (int u = lane; u < (H_q + 2 * H_kv) * CPH; u += 64) {
-        const int h = u / CPH, e0 = u % CPH * 8;
-        const int hk = h - H_q, hv = hk - H_kv;
-        if (hk >= 0 && !stored) continue;
-        const bf16_t* src = hk < 0 ? q + r * st_q + h * D_H : hv < 0 ? k + r * st_k + hk * D_H : v + r * st_v + hv * D_H;
-        bf16_t* dst = hk < 0 ? q_out + ((int64_t)r * H_q + h) * D_H : (hv < 0 ? Kp + slot + hk * st_head : Vp + slot + hv * st_head);
-        bf16_t x[8], y[8];
+    constexpr int NC = MODE == ROPE_NEIGHBOURS ? 4 : 8;
+    float2 c[NC];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = src[e0 + e];
-        if (hv < 0) {
+    for (int e = 0; e < NC; ++e) {
+        const int j = MODE == ROPE_NEIGHBOURS ? e0 / 2 + e : MODE == ROPE_HALVES ? e0 + e : (e0 + e) % half;
+        c[e] = cs[w][min(j, half - 1)];
+    }
+    for (int hb = h0; hb < h_end; hb += NB * per_pass) {
+        if (hb != h0) load(hb);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = e0 + e;
-                const int other = i >= a.rot ? i : a.interleaved ? i ^ 1 : i < half ? i + half : i - half;
-                y[e] = src[other];
+        for (int i = 0; i < NB; ++i) {
+            const int h = hb + i * per_pass, hk = h - H_q, hv = hk - H_kv;
+            if (h >= h_end || (hk >= 0 && !stored)) continue;
+            bf16_t* dst = (hk < 0 ? q_out + ((int64_t)r * H_q + h) * D_H : hv < 0 ? Kp + slot + hk * st_head : Vp + slot + hv * st_head) + e0;
+            if (hv < 0) {
+                if (MODE == ROPE_HALVES && paired) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float lo = (float)x[i][e], hi = (float)y[i][e];
+                        x[i][e] = (bf16_t)(lo * c[e].x - hi * c[e].y);
+                        y[i][e] = (bf16_t)(hi * c[e].x + lo * c[e].y);
+                    }
+                } else if (MODE == ROPE_NEIGHBOURS) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float lo = (float)x[i][2 * e], hi = (float)x[i][2 * e + 1];
+                        if (e0 + 2 * e < a.rot) {
+                            x[i][2 * e] = (bf16_t)(lo * c[e].x - hi * c[e].y);
+                            x[i][2 * e + 1] = (bf16_t)(hi * c[e].x + lo * c[e].y);
+                        }
+                    }
+                } else if (MODE == ROPE_ODD_HALVES) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int j = e0 + e;
+                        const float m = (float)x[i][e] * c[e].x, o = (float)y[i][e] * c[e].y;
+                        if (j < a.rot) x[i][e] = (bf16_t)(j < half ? m - o : m + o);
+                    }
+                }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = e0 + e;
-                if (i >= a.rot) continue;
-                const float2 c = cs[w][a.interleaved ? i >> 1 : i < half ? i : i - half];
-                const bool first = a.interleaved ? (i & 1) == 0 : i < half;
-                const float m = (float)x[e] * c.x, o = (float)y[e] * c.y;
-                x[e] = (bf16_t)(first ? m - o : m + o);
-            }
+            *reinterpret_cast<bf16x8*>(dst) = x[i];
+            if (MODE == ROPE_HALVES && paired) *reinterpret_cast<bf16x8*>(dst + half) = y[i];
         }
-        bf16x8 out;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = x[e];
-        *reinterpret_cast<bf16x8*>(dst + e0) = out;
     }
 }
 
@@ -416,13 +466,25 @@ void cc_launch_rope_append(const bf16_t* q, int64_t st_q, const bf16_t* k, int64
     a.rot = rope.rot;
     a.interleaved = rope.interleaved != 0;
     a.mscale = (float)rope.mscale;
-    const dim3 grid((r.rows + 3) / 4);
-    if (m.d_h == 128)
-        hipLaunchKernelGGL(rope_append_kernel<128>, grid, dim3(256), 0, s, a, q, st_q, k, st_k, v, st_v, r.start, r.seq, r.n, r.rows,
-                           pos, cc_view(p), (bf16_t*)kv.K, (bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, m.H_q,
-                           m.H_kv, q_out);
-    else
-        hipLaunchKernelGGL(rope_append_kernel<64>, grid, dim3(256), 0, s, a, q, st_q, k, st_k, v, st_v, r.start, r.seq, r.n, r.rows,
-                           pos, cc_view(p), (bf16_t*)kv.K, (bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, m.H_q,
-                           m.H_kv, q_out);
+    // slices of a row until there are sixteen waves a CU or every pass has a wave of its own
+    const int mode = a.interleaved ? ROPE_NEIGHBOURS : a.rot % 16 ? ROPE_ODD_HALVES : ROPE_HALVES;
+    const int units = mode == ROPE_HALVES ? m.d_h / 8 - a.rot / 16 : m.d_h / 8, per_pass = 64 / units;
+    const int passes = (m.H_q + 2 * m.H_kv + per_pass - 1) / per_pass;
+    const int slices = std::max(1, std::min(passes, 16 * cc_device_cus() / r.rows));
+    const int per_slice = (passes + slices - 1) / slices;
+    const dim3 grid((r.rows + 3) / 4, (passes + per_slice - 1) / per_slice);
+#define CC_ROPE(D, MODE)                                                                                                   \
+    hipLaunchKernelGGL((rope_append_kernel<D, MODE>), grid, dim3(256), 0, s, a, q, st_q, k, st_k, v, st_v, r.start, r.seq, r.n, r.rows, \
+                       pos, cc_view(p), (bf16_t*)kv.K, (bf16_t*)kv.V, kv.stride_page, kv.stride_token, kv.stride_head, m.H_q,  \
+                       m.H_kv, q_out, per_slice)
+    if (m.d_h == 128) {
+        if (mode == ROPE_HALVES) CC_ROPE(128, ROPE_HALVES);
+        else if (mode == ROPE_NEIGHBOURS) CC_ROPE(128, ROPE_NEIGHBOURS);
+        else CC_ROPE(128, ROPE_ODD_HALVES);
+    } else {
+        if (mode == ROPE_HALVES) CC_ROPE(64, ROPE_HALVES);
+        else if (mode == ROPE_NEIGHBOURS) CC_ROPE(64, ROPE_NEIGHBOURS);
+        else CC_ROPE(64, ROPE_ODD_HALVES);
+    }
+#undef CC_ROPE
 }
