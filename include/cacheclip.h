@@ -276,7 +276,7 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
  *   work    cc_page_work_bytes(n_pages, n_seqs) bytes, 256-byte aligned: scratch, its contents mean nothing
  *           between calls.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
  *           at once), whatever context they come from.
- * page_size is a power of two, 16 to 1024; n_seqs <= 65536, n_pages * page_size < 2^31. */
+ * page_size is a power of two, 16 to 1024; n_seqs <= 65536, n_pages * page_size < 2^31, max_pages * page_size < 2^30. */
 typedef struct cc_page_pool {
     int32_t* refs;
     int32_t* table;
@@ -294,7 +294,7 @@ int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs);
 
 /* One layer's pages, dev bf16: element (page, token, head, c) of K and V is at
  * page*stride_page + token*stride_token + head*stride_head + c (elements; strides multiples of 8, c contiguous,
- * tokens or heads outermost in a page).  Slots behind a sequence's last token may hold anything; the others must be
+ * tokens or heads outermost in a page, stride_token < 2^23).  Slots behind a sequence's last token may hold anything; the others must be
  * finite, as everywhere in this library.  A page outside [0, n_pages) reads as zeros and is never written, so that
  * pages which slid out of every window may be given back. */
 typedef struct cc_paged_kv {
@@ -308,7 +308,7 @@ typedef struct cc_paged_kv {
 /* New tokens of a batch: rows start[b] .. start[b+1]-1 of q, k, v and o are the last tokens of sequence
  * seq[b] (b itself where seq is NULL); row r sits at position len - (start[b+1] - start[b]) + r - start[b], its length
  * already counts it (cc_grow_pages).  A sequence without rows is allowed.  Rows that belong to no sequence
- * (in front of start[0], behind start[n]) are neither read nor written. */
+ * (in front of start[0], behind start[n]) are not written. */
 typedef struct cc_new_rows {
     const int32_t* start;   /* dev [n + 1], ascending, within [0, rows] */
     const int32_t* seq;     /* dev [n], each in [0, n_seqs), or NULL */

@@ -111,6 +111,10 @@ __device__ __forceinline__ float2 get(const float* p) {
     const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char* scalar_base(const char* p) {
+    return (const char*)uniform((int64_t)(uintptr_t)p);
+}
 
 // Key tiles of `keys` keys that the rows of a sequence see: the first `sink` tiles, then those from `from` to the end.
 struct tile_span {

@@ -24,6 +24,9 @@ namespace {
 constexpr int KEYS = 32;                      // of a tile of few_attn_kernel
 constexpr int WAVES = 4;
 constexpr int START = 4;                      // units that a block costs besides its tiles: its queries, first loads and result
+// Blocks of up to so many tiles are not cut where every block can have a workgroup: 512 tokens take 8.3 us either way, 256
+// take 6.2 whole and 7.3 in pieces (one sequence, 4 query heads of 2, d_h 64), 7.0 and 8.6 (32 of 8, d_h 128).
+constexpr int WHOLE = 16;
 
 // 16 bytes per lane from global memory into LDS at wave base + OFF + 16 * lane; OFF is added to the global address too.
 // Non-temporal: what few rows read is read once.
@@ -38,9 +41,6 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
     asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ const char* scalar_ptr(const char* p) {
-    return (const char*)uniform((int64_t)(uintptr_t)p);
 }
 
 struct paged_args {
@@ -74,6 +74,18 @@ __device__ __forceinline__ batch_seq seq_of(const paged_args& a, int b) {
     return r;
 }
 
+// The value, where it is asked for: what is made of it is not made ahead and kept through the loop in front of it.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ int64_t of_lane(int64_t v, int l) {
+    return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, l);
+}
+// x / y of whole numbers, 0 <= x < 2^52: the quotient in 64-bit floating point is exact enough to be cut off, and takes a
+// tenth of the instructions of a 64-bit integer division.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) { return (int64_t)((double)x / (double)y); }
+
 // NC: blocks of 16 columns that a wave multiplies a tile with.  Compiled for workgroups of eight waves, two a SIMD: with 512 registers the
 // compiler keeps the sums in accumulation registers and copies them out and in for every rescale.
 template <int D_H, int NC>
@@ -89,35 +101,50 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
     constexpr int NS = D_H == 128 ? 2 : 4;    // tiles in a wave's ring
     constexpr int RING = 2 * NS * TILE;
     constexpr int COLS = 16 * NC;
-    constexpr bool Q_LDS = NC * KS > 8;       // the queries' fragments do not fit the registers
     __shared__ __align__(1024) char ring[WAVES][RING];
     __shared__ int64_t pre[CC_PAGED_MAX_N + 1];
     __shared__ int64_t wave_sum[WAVES];
     __shared__ float2 ml[WAVES][COLS];
-    __shared__ bf16x8 qs[Q_LDS ? NC : 1][Q_LDS ? KS : 1][64];
     __shared__ int last_here;
     static_assert(COLS * D_H * 4 <= RING, "a wave's sums fit its ring");
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
-    const int c16 = lane & 15, kg = lane >> 4;
 
-    // ---- units before every sequence of the batch ----
-    {
+    // ---- units in front of every sequence of the batch: up to 64 sequences a lane each, in every wave; more in LDS ----
+    auto blocks_of = [&](const batch_seq& s) -> int { return (s.n * a.g + COLS - 1) / COLS * a.H_kv; };
+    auto block_len = [&](const batch_seq& s) -> int {
+        return s.n > 0 ? visible_tiles(s.L - s.n, s.L, a.window, a.sinks, KEYS).count + START : 0;
+    };
+    // over the first `lanes` lanes: an exchange between lanes is a trip through LDS, and one sequence needs none
+    auto wave_scan = [&](int64_t v, int lanes) -> int64_t {
+        for (int off = 1; off < lanes; off <<= 1) {
+            const int64_t x = __shfl_up(v, off);
+            if (lane >= off) v += x;
+        }
+        return v;
+    };
+    const bool small = a.n <= 64;
+    batch_seq mine = {0, 0, 0, 0};
+    int64_t my_end = 0, my_units = 0, total;
+    int whole_len = 0;        // > 0: no block is cut, and each is as long as the longest
+    if (small) {
+        mine = seq_of(a, min(lane, a.n - 1));
+        if (lane >= a.n) mine.n = 0;
+        int len = block_len(mine), longest = len, blocks = blocks_of(mine);
+        for (int off = 1; off < a.n; off <<= 1) {
+            longest = max(longest, __shfl_xor(longest, off));
+            blocks += __shfl_xor(blocks, off);
+        }
+        longest = uniform(longest);
+        if (longest <= WHOLE + START && uniform(blocks) <= (int)gridDim.x) whole_len = len = longest;
+        my_units = (int64_t)blocks_of(mine) * len;
+        my_end = wave_scan(my_units, a.n);
+        total = of_lane(my_end, a.n - 1);
+    } else {
         int64_t carry = 0;
         for (int i0 = 0; i0 < a.n; i0 += 64 * WAVES) {
             const int i = i0 + tid;
-            int64_t u = 0;
-            if (i < a.n) {
-                const batch_seq s = seq_of(a, i);
-                if (s.n > 0) {
-                    const tile_span v = visible_tiles(s.L - s.n, s.L, a.window, a.sinks, KEYS);
-                    u = (int64_t)((s.n * a.g + COLS - 1) / COLS) * a.H_kv * (v.count + START);
-                }
-            }
-            int64_t inc = u;
-            for (int off = 1; off < 64; off <<= 1) {
-                const int64_t v = __shfl_up(inc, off);
-                if (lane >= off) inc += v;
-            }
+            const batch_seq s = seq_of(a, min(i, a.n - 1));
+            const int64_t v = i < a.n ? (int64_t)blocks_of(s) * block_len(s) : 0, inc = wave_scan(v, 64);
             if (lane == 63) wave_sum[w] = inc;
             __syncthreads();
             int64_t base = carry;
@@ -125,93 +152,75 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                 if (j < w) base += wave_sum[j];
                 carry += wave_sum[j];
             }
-            if (i < a.n) pre[i] = base + inc - u;
+            if (i < a.n) pre[i] = base + inc - v;
             __syncthreads();
         }
         if (tid == 0) pre[a.n] = carry;
         __syncthreads();
+        total = uniform(pre[a.n]);
     }
-    const int64_t total = uniform(pre[a.n]);
-    const int64_t per = max((int64_t)per_min, (total + gridDim.x - 1) / gridDim.x);
+    const int64_t per = whole_len > 0 ? whole_len : max((int64_t)per_min, quotient(total + gridDim.x - 1, gridDim.x));
     const int range = blockIdx.x;
     int64_t u = range * per;
     const int64_t stop = min(u + per, total);
 
-    // ---- lane constants: loads (row and swizzled chunk) and fragment addresses ----
-    // K: chunk c of row r at slot c ^ kswz(r); V: the 32-byte pair of chunks dt at pair dt ^ vswz(r).
-    auto kswz = [](int r) { return D_H == 128 ? (r & 15) : ((r >> 1) & 7); };
-    auto vswz = [](int r) { return D_H == 128 ? (r & 7) : ((r >> 1) & 3); };
-    const int l_row = lane / CPR, l_c = lane % CPR;
-    const uint32_t st_b = (uint32_t)a.st_tok * 2;
-    uint32_t k_off[HL], v_off[HL];                        // from the first of 16 rows, of the lane's 16 bytes of load i
-#pragma unroll
-    for (int i = 0; i < HL; ++i) {
-        const int r = i * RPI + l_row;
-        k_off[i] = r * st_b + (l_c ^ kswz(r)) * 16;
-        v_off[i] = r * st_b + (l_c ^ (2 * vswz(r))) * 16;
-    }
-    char* const my_ring = ring[w];
-    const uint32_t ring_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)my_ring;
-    uint32_t kaddr[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kaddr[ks] = ring_at + c16 * ROW + (((ks * 4 + kg) ^ kswz(c16)) << 4);
-    const int v_row = 4 * kg + (c16 >> 2);
-    const uint32_t v_base = ring_at + TILE + v_row * ROW + ((((c16 & 3) >> 1) ^ (2 * vswz(v_row))) << 4) + (c16 & 1) * 8;
-    uint32_t vaddr[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) vaddr[dt] = v_base ^ (dt << 5);
-
-    const uint32_t q_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)&qs[0][0][lane];
-
     while (u < stop) {
         // ---- the block that unit u lies in ----
-        int b = 0;
-        for (int i = lane; i - lane < a.n; i += 64) b += __popcll(__ballot(i < a.n && pre[min(i, a.n - 1) + 1] <= u));
-        b = uniform(b);
-        const batch_seq sq = seq_of(a, b);
-        const int row0 = uniform(sq.row0), n_new = uniform(sq.n), s = uniform(sq.s), L = uniform(sq.L);
+        int row0, n_new, s, L;
+        int64_t seq0;
+        if (small) {
+            const int b = __popcll(__ballot(lane < a.n && my_end <= u));
+            row0 = __builtin_amdgcn_readlane(mine.row0, b);
+            n_new = __builtin_amdgcn_readlane(mine.n, b);
+            s = __builtin_amdgcn_readlane(mine.s, b);
+            L = __builtin_amdgcn_readlane(mine.L, b);
+            seq0 = of_lane(my_end - my_units, b);
+        } else {
+            int b = 0;
+            for (int i = lane; i - lane < a.n; i += 64) b += __popcll(__ballot(i < a.n && pre[min(i, a.n - 1) + 1] <= u));
+            b = uniform(b);
+            const batch_seq sq = seq_of(a, b);
+            row0 = uniform(sq.row0), n_new = uniform(sq.n), s = uniform(sq.s), L = uniform(sq.L);
+            seq0 = uniform(pre[b]);
+        }
         const int first = L - n_new;
         const tile_span span = visible_tiles(first, L, a.window, a.sinks, KEYS);
-        const int64_t seq0 = uniform(pre[b]);
-        const int len = span.count + START;
-        const int which = (int)((u - seq0) / len), blk = which / a.H_kv, h = which - blk * a.H_kv;
+        const int len = whole_len > 0 ? whole_len : span.count + START;
+        const int which = (int)quotient(u - seq0, len), blk = which / a.H_kv, h = which - blk * a.H_kv;
         const int64_t u0 = seq0 + (int64_t)which * len, u1 = u0 + len;
-        const int ta = (int)max((int64_t)0, u - u0 - START), te = (int)(min(u1, stop) - u0 - START);
-        const bool opened_here = u0 + START >= range * per;
+        const int ta = (int)max((int64_t)0, u - u0 - START), te = min((int)(min(u1, stop) - u0) - START, span.count);
         u = u1;
         if (te <= ta) continue;
 
+        // ---- lane constants of the block: loads (row and swizzled chunk) and fragment addresses ----
+        // K: chunk c of row r at slot c ^ kswz(r); V: the 32-byte pair of chunks dt at pair dt ^ vswz(r).
+        auto kswz = [](int r) { return D_H == 128 ? (r & 15) : ((r >> 1) & 7); };
+        auto vswz = [](int r) { return D_H == 128 ? (r & 7) : ((r >> 1) & 3); };
+        const int ln0 = here(lane), c16 = ln0 & 15, kg = ln0 >> 4, l_row = ln0 / CPR, l_c = ln0 % CPR;
+        // Both swizzles and the places they act on are bit fields: what a load's index, a k-step or a tile of O^T adds to an address
+        // is one exclusive or with a constant.
+        const uint32_t st_b = (uint32_t)a.st_tok * 2;
+        const uint32_t k_col = (l_c ^ kswz(l_row)) * 16, v_col = (l_c ^ (2 * vswz(l_row))) * 16;
+        char* const my_ring = ring[w];
+        const uint32_t ring_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)my_ring;
+        const uint32_t k_base = ring_at + c16 * ROW + ((kg ^ kswz(c16)) << 4);
+        const int v_row = 4 * kg + (c16 >> 2);
+        const uint32_t v_base = ring_at + TILE + v_row * ROW + ((((c16 & 3) >> 1) ^ (2 * vswz(v_row))) << 4) + (c16 & 1) * 8;
+
         // ---- queries: B operand of the scores ----
-        bf16x8 qf[Q_LDS ? 1 : NC][KS];
-        int limit[NC], under[NC];                          // the newest key a column sees; keys up to `under` left its window
-        int most = -1, least = 0x7fffffff;                 // positions of the block's rows
+        bf16x8 qf[NC][KS];
+        int limit[NC];                                     // the newest key a column sees
+        // positions of the block's last and first row
+        const int most = max(first + min(n_new - 1, (blk * COLS + COLS - 1) / a.g), -1), least = max(first + blk * COLS / a.g, -1);
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc) {
             const int col = blk * COLS + nc * 16 + c16, i = col / a.g, hg = col - i * a.g;
             const bool valid = i < n_new;
             limit[nc] = valid ? max(first + i, -1) : -1;
-            under[nc] = a.window > 0 ? limit[nc] - a.window : (int)0x80000000;
-            most = max(most, limit[nc]);
-            if (valid) least = min(least, limit[nc]);
             const bf16_t* qp = a.q + ((int64_t)(row0 + (valid ? i : 0)) * a.H_q + h * a.g + (valid ? hg : 0)) * D_H + 8 * kg;
-            if constexpr (Q_LDS) {
-                if (nc == w) {
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) qs[nc][ks][lane] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
-                }
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) qf[nc][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
-            }
+            for (int ks = 0; ks < KS; ++ks) qf[nc][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
         }
-        if constexpr (Q_LDS) __syncthreads();
-        for (int off = 8; off > 0; off >>= 1) {
-            most = max(most, __shfl_xor(most, off));
-            least = min(least, __shfl_xor(least, off));
-        }
-        most = uniform(most);
-        least = uniform(least);
-
         f32x4 acc[DT][NC];
         float m_run[NC], l_run[NC];
 #pragma unroll
@@ -228,10 +237,10 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         // (scalar loads do not count among the loads that the waits below count)
         const in_pages::table_t row_table = (in_pages::table_t)(a.p.table + s * a.p.st_table);
         const int64_t head_off = (int64_t)h * a.st_head;
-        // The two pages of a tile (16 keys each, in one page), asked for a tile ahead of the loads that need them.
+        // The two pages of a tile (16 keys each, in one page): those of the first NS tiles together, the others' a tile ahead.
         struct pages { int a, b; };
         auto pages_of = [&](int k) __attribute__((always_inline)) -> pages {
-            const int key0 = tile_key(k), end = max(L - 1, 0);
+            const int key0 = tile_key(min(k, max(nt - 1, 0))), end = max(L - 1, 0);
             return {row_table[min(key0, end) >> a.p.shift], row_table[min(key0 + 16, end) >> a.p.shift]};
         };
         // First row of 16 keys as an offset into K and V, and its last one: rows behind the last token repeat it (they are
@@ -243,43 +252,22 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                     there ? min(15, L - 1 - key0) : -1};
         };
         // (a scalar base and a 32-bit lane offset: 64-bit vector addresses cost more to make than the loads to issue)
-        auto load = [&](const bf16_t* base, rows16 r, const uint32_t* off16, char* dst) __attribute__((always_inline)) {
-            const char* src = (const char*)base + r.at;
-            if (r.rmax == 15) {
-                static_for<HL>([&](auto ic) __attribute__((always_inline)) {
-                    constexpr int i = decltype(ic)::value;
-                    uint32_t off = off16[i];
-                    asm volatile("" : "+v"(off));
-                    stream16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
-                });
-            } else {
-                if (r.rmax < 0) src = (const char*)a.zeros;
-                static_for<HL>([&](auto ic) __attribute__((always_inline)) {
-                    constexpr int i = decltype(ic)::value;
-                    const int row = i * RPI + l_row;
-                    uint32_t off = off16[i] - (uint32_t)(row - min(row, max(r.rmax, 0))) * st_b;
-                    asm volatile("" : "+v"(off));
-                    stream16<i * 1024>(scalar_ptr(src - i * 1024) + off, dst);
-                });
-            }
+        auto load = [&](const bf16_t* base, rows16 r, uint32_t col, auto swz, char* dst) __attribute__((always_inline)) {
+            const char* src = r.rmax < 0 ? (const char*)a.zeros : (const char*)base + r.at;
+            const int last = max(r.rmax, 0);
+            static_for<HL>([&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                uint32_t off = __umul24(min(i * RPI + l_row, last), st_b) + (col ^ (swz(i * RPI) << 4));
+                asm volatile("" : "+v"(off));
+                stream16<i * 1024>(scalar_base(src - i * 1024) + off, dst);
+            });
         };
-        auto stage_of = [&](int k) { return my_ring + (k % NS) * 2 * TILE; };
-        {
-            pages pg[NS];
+        auto kswz_of = [&](int r) { return kswz(r); };
+        auto vswz_of = [&](int r) { return 2 * vswz(r); };
+        auto stage_of = [&](int k) { return my_ring + ((k + NS) % NS) * 2 * TILE; };
+        pages ahead[NS];
 #pragma unroll
-            for (int k = 0; k < NS; ++k) pg[k] = pages_of(min(k, max(nt - 1, 0)));
-#pragma unroll
-            for (int k = 0; k < NS; ++k)
-                if (k < nt) {
-                    const int key0 = tile_key(k);
-                    const rows16 x = rows_of(key0, pg[k].a), y = rows_of(key0 + 16, pg[k].b);
-                    load(a.K, x, k_off, stage_of(k));
-                    load(a.K, y, k_off, stage_of(k) + TILE / 2);
-                    load(a.V, x, v_off, stage_of(k) + TILE);
-                    load(a.V, y, v_off, stage_of(k) + TILE + TILE / 2);
-                }
-        }
-        pages pg_next = pages_of(max(0, min(NS, nt - 1)));
+        for (int k = 0; k < NS; ++k) ahead[k] = pages_of(k);
         // Loads younger than K(k): V(k) and the pairs of up to NS - 1 later tiles; than V(k): those and K(k + NS).
         auto wait_k = [&](int rem) __attribute__((always_inline)) {
             static_for<NS>([&](auto jc) __attribute__((always_inline)) {
@@ -295,70 +283,72 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             if (rem >= NS) wait_loads<NL * (2 * (NS - 1) + 1)>();
         };
 
-        for (int k = 0; k < nt; ++k) {
-            const int key0 = tile_key(k), rem = nt - 1 - k;
-            const uint32_t stage = (uint32_t)(k % NS) * 2 * TILE;
-            wait_k(rem);
+        // Iterations -NS .. -1 only fill the ring.
+#pragma unroll 1
+        for (int k = -NS; k < nt; ++k) {
+            const int key0 = tile_key(k), rem = nt - 1 - k, key_in = tile_key(k + NS);
+            const uint32_t stage = (uint32_t)((k + NS) % NS) * 2 * TILE;
             bf16x8 kf[2][KS];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                kf[0][ks] = lds_read_b128_at<0>(kaddr[ks] + stage);
-                kf[1][ks] = lds_read_b128_at<16 * ROW>(kaddr[ks] + stage);
+            if (k >= 0) {
+                wait_k(rem);
+                static_for<KS>([&](auto kc) __attribute__((always_inline)) {
+                    constexpr int ks = decltype(kc)::value;
+                    const uint32_t at = (k_base + stage) ^ (ks << 6);
+                    kf[0][ks] = lds_read_b128_at<0>(at);
+                    kf[1][ks] = lds_read_b128_at<16 * ROW>(at);
+                });
+                if constexpr (KS == 4)
+                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1]), "+v"(kf[0][2]),
+                                 "+v"(kf[1][2]), "+v"(kf[0][3]), "+v"(kf[1][3])
+                                 :: "memory");
+                else
+                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1])::"memory");
             }
-            if constexpr (KS == 4)
-                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1]), "+v"(kf[0][2]),
-                             "+v"(kf[1][2]), "+v"(kf[0][3]), "+v"(kf[1][3])
-                             :: "memory");
-            else
-                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kf[0][0]), "+v"(kf[1][0]), "+v"(kf[0][1]), "+v"(kf[1][1])::"memory");
-            const rows16 x = rows_of(tile_key(k + NS), pg_next.a), y = rows_of(tile_key(k + NS) + 16, pg_next.b);
+            const rows16 x = rows_of(key_in, ahead[0].a), y = rows_of(key_in + 16, ahead[0].b);
             if (rem >= NS) {
-                load(a.K, x, k_off, stage_of(k));
-                load(a.K, y, k_off, stage_of(k) + TILE / 2);
+                load(a.K, x, k_col, kswz_of, stage_of(k));
+                load(a.K, y, k_col, kswz_of, stage_of(k) + TILE / 2);
             }
-            f32x4 sc[NC][2];
+#pragma unroll
+            for (int i = 0; i + 1 < NS; ++i) ahead[i] = ahead[i + 1];
+            if (k < 0) {
+                if (k == -1) ahead[0] = pages_of(NS);
+                if (rem >= NS) {
+                    load(a.V, x, v_col, vswz_of, stage_of(k) + TILE);
+                    load(a.V, y, v_col, vswz_of, stage_of(k) + TILE + TILE / 2);
+                }
+                continue;
+            }
+            // a block of columns at a time: scores, mask, softmax in base 2 with the scale folded into the exponent
+            const bool masked = key0 + KEYS - 1 > least || (a.window > 0 && key0 <= most - a.window && key0 + KEYS > a.sinks);
+            bf16x8 pf[NC];
 #pragma unroll
             for (int nc = 0; nc < NC; ++nc) {
-                if constexpr (Q_LDS) {
-                    static_assert(!Q_LDS || KS == 4, "four fragments a column block");
-                    const uint32_t at = q_at + nc * KS * 1024;
-                    qf[0][0] = lds_read_b128_at<0>(at);
-                    qf[0][1] = lds_read_b128_at<1024>(at);
-                    qf[0][KS - 2] = lds_read_b128_at<(KS - 2) * 1024>(at);
-                    qf[0][KS - 1] = lds_read_b128_at<(KS - 1) * 1024>(at);
-                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(qf[0][0]), "+v"(qf[0][1]), "+v"(qf[0][KS - 2]), "+v"(qf[0][KS - 1]));
-                }
+                f32x4 sc[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    sc[nc][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        sc[nc][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][ks], qf[Q_LDS ? 0 : nc][ks], sc[nc][t], 0, 0, 0);
+                        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][ks], qf[nc][ks], sc[t], 0, 0, 0);
                 }
-            }
-            // ---- mask: keys behind a row, or in front of its window and no sink ----
-            if (key0 + KEYS - 1 > least || (a.window > 0 && key0 <= most - a.window && key0 + KEYS > a.sinks)) {
-#pragma unroll
-                for (int nc = 0; nc < NC; ++nc)
+                if (masked) {                              // keys behind a row, or in front of its window and no sink
+                    const int under = a.window > 0 ? limit[nc] - a.window : (int)0x80000000;
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
                             const int key = key0 + t * 16 + 4 * kg + v;
                             // (no short circuits: selects, not branches)
-                            const bool out = (key > limit[nc]) | ((key <= under[nc]) & (key >= a.sinks));
-                            sc[nc][t][v] = out ? -INFINITY : sc[nc][t][v];
+                            const bool out = (key > limit[nc]) | ((key <= under) & (key >= a.sinks));
+                            sc[t][v] = out ? -INFINITY : sc[t][v];
                         }
-            }
-            // ---- softmax in base 2, the scale folded into the exponent ----
-            bf16x8 pf[NC];
-#pragma unroll
-            for (int nc = 0; nc < NC; ++nc) {
+                }
                 float mx = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[nc][t][v]);
+                    for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[t][v]);
                 mx *= a.scale_log2;
                 if (__any(mx > m_run[nc] + 8.0f)) {
                     mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -375,7 +365,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[nc][t][v], a.scale_log2, -ref));
+                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[t][v], a.scale_log2, -ref));
                         l_run[nc] += p;
                         pf[nc][t * 4 + v] = (bf16_t)p;
                     }
@@ -383,21 +373,22 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             // ---- O^T += V^T P^T: the 32 keys in the order in which a lane holds its scores ----
             wait_v(rem);
             bf16x4 va[DT], vb[DT];
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                va[dt] = lds_read_tr_at<0>(vaddr[dt] + stage);
-                vb[dt] = lds_read_tr_at<16 * ROW>(vaddr[dt] + stage);
-            }
+            static_for<DT>([&](auto dc) __attribute__((always_inline)) {
+                constexpr int dt = decltype(dc)::value;
+                const uint32_t at = (v_base + stage) ^ (dt << 5);
+                va[dt] = lds_read_tr_at<0>(at);
+                vb[dt] = lds_read_tr_at<16 * ROW>(at);
+            });
             asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(vb[0]), "+v"(va[1]), "+v"(vb[1]), "+v"(va[2]), "+v"(vb[2]),
                          "+v"(va[3]), "+v"(vb[3])
                          :: "memory");
             if constexpr (DT == 8)
                 asm volatile("" : "+v"(va[4]), "+v"(vb[4]), "+v"(va[5]), "+v"(vb[5]), "+v"(va[6]), "+v"(vb[6]), "+v"(va[7]), "+v"(vb[7])::"memory");
             if (rem >= NS) {
-                load(a.V, x, v_off, stage_of(k) + TILE);
-                load(a.V, y, v_off, stage_of(k) + TILE + TILE / 2);
+                load(a.V, x, v_col, vswz_of, stage_of(k) + TILE);
+                load(a.V, y, v_col, vswz_of, stage_of(k) + TILE + TILE / 2);
             }
-            pg_next = pages_of(min(k + 1 + NS, nt - 1));
+            ahead[0] = pages_of(k + 1 + NS);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const bf16x8 vf = __builtin_shufflevector(va[dt], vb[dt], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -407,92 +398,118 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             }
         }
 
-        // ---- the four waves' sums together: as the registers lie, [dt][nc][lane] ----
+        // ---- the four waves' sums together, as the registers lie: [dt][nc][lane]; to the output or to a piece (two lots of
+        // eight bytes a lane, then (maximum, sum) a column).  Ends with the rings free again ----
+        auto together = [&](float* piece) __attribute__((always_inline)) {
+            const int ln = here(lane), c = ln & 15, quad = ln >> 4;
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc) {
+                float l = l_run[nc];
+                l += __shfl_xor(l, 16);
+                l += __shfl_xor(l, 32);
+                if (quad == 0) ml[w][nc * 16 + c] = make_float2(m_run[nc], l);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+                    *reinterpret_cast<f32x4*>(my_ring + ((dt * NC + nc) * 64 + ln) * 16) = acc[dt][nc];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc) {
+                float2 x[WAVES];
+                float m = -INFINITY, l = 0.0f;
+#pragma unroll
+                for (int j = 0; j < WAVES; ++j) {
+                    x[j] = ml[j][nc * 16 + c];
+                    m = fmaxf(m, x[j].x);
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int j = 0; j < WAVES; ++j) {
+                    x[j].x = __builtin_amdgcn_exp2f(x[j].x - ref);
+                    l += x[j].x * x[j].y;
+                }
+                const int col = blk * COLS + nc * 16 + c, i = col / a.g, hg = col - i * a.g;
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+                for (int d = 0; d < DT / WAVES; ++d) {
+                    const int dt = d * WAVES + w;
+                    f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < WAVES; ++j)
+                        r += x[j].x * *reinterpret_cast<const f32x4*>(ring[j] + ((dt * NC + nc) * 64 + ln) * 16);
+                    if (piece) {
+                        put(piece + (dt * NC + nc) * 256 + ln * 2, r[0], r[1]);
+                        put(piece + (dt * NC + nc) * 256 + 128 + ln * 2, r[2], r[3]);
+                    } else if (i < n_new) {
+                        bf16x4 out;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) out[e] = (bf16_t)(r[e] * inv);
+                        *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * quad) = out;
+                    }
+                }
+                if (piece && w == 0 && quad == 0) put(piece + COLS * D_H + nc * 32 + c * 2, m, l);
+            }
+            if (piece) wait_loads<0>();                    // it is written
+            __syncthreads();
+        };
+        // ---- A cut block: a range leaves at most two pieces, of the block it starts in and of a later one.  The workgroup
+        // that comes last adds them: a wave takes every fourth, then as above.  (Stores past the L2 have been
+        // acknowledged before the count is raised, and loads past it follow the count: no fence is needed.) ----
+        const int w0 = (int)quotient(u0 + START, per), w1 = (int)quotient(u1 - 1, per);
+        auto piece_of = [&](int j) { return a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * COLS * (D_H + 2); };
         wait_loads<0>();
-#pragma unroll
-        for (int nc = 0; nc < NC; ++nc) {
-            float l = l_run[nc];
-            l += __shfl_xor(l, 16);
-            l += __shfl_xor(l, 32);
-            if (kg == 0) ml[w][nc * 16 + c16] = make_float2(m_run[nc], l);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-                *reinterpret_cast<f32x4*>(my_ring + ((dt * NC + nc) * 64 + lane) * 16) = acc[dt][nc];
-        }
-        __syncthreads();
-        const bool whole = ta == 0 && te == span.count;
-        // pieces: a range leaves at most two, of the block it starts in and of a later one
-        float* const piece = a.part + (int64_t)(2 * range + (opened_here ? 1 : 0)) * COLS * (D_H + 2);
-#pragma unroll
-        for (int nc = 0; nc < NC; ++nc) {
-            float2 x[WAVES];
-            float m = -INFINITY, l = 0.0f;
-#pragma unroll
-            for (int j = 0; j < WAVES; ++j) {
-                x[j] = ml[j][nc * 16 + c16];
-                m = fmaxf(m, x[j].x);
+        float* piece = ta == 0 && te == span.count ? nullptr : piece_of(range);
+        while (true) {
+            together(piece);
+            if (!piece) break;
+            if (tid == 0) {
+                const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                last_here = before == w1 - w0;
+                if (last_here) __hip_atomic_store(&a.arrived[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
-            const float ref = m == -INFINITY ? 0.0f : m;
+            __syncthreads();
+            if (!last_here) break;
+            piece = nullptr;
+            const int ln = here(lane), c = ln & 15, quad = ln >> 4;
 #pragma unroll
-            for (int j = 0; j < WAVES; ++j) {
-                x[j].x = __builtin_amdgcn_exp2f(x[j].x - ref);
-                l += x[j].x * x[j].y;
+            for (int nc = 0; nc < NC; ++nc) {
+                m_run[nc] = -INFINITY;
+                l_run[nc] = 0.0f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) acc[dt][nc] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            const int col = blk * COLS + nc * 16 + c16, i = col / a.g, hg = col - i * a.g;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            for (int dt = w; dt < DT; dt += WAVES) {
-                f32x4 r = {0.f, 0.f, 0.f, 0.f};
+            constexpr int AT_ONCE = NC == 1 ? 2 : 1;
+            for (int j = w0 + w; j <= w1; j += WAVES * AT_ONCE) {
 #pragma unroll
-                for (int j = 0; j < WAVES; ++j)
-                    r += x[j].x * *reinterpret_cast<const f32x4*>(ring[j] + ((dt * NC + nc) * 64 + lane) * 16);
-                if (!whole) {
-                    put(piece + ((dt * NC + nc) * 128 + lane) * 2, r[0], r[1]);
-                    put(piece + ((dt * NC + nc) * 128 + 64 + lane) * 2, r[2], r[3]);
-                } else if (i < n_new) {
-                    bf16x4 out;
+                for (int nc = 0; nc < NC; ++nc) {
+                    float2 x[AT_ONCE], v[AT_ONCE][DT][2];
+                    float m = m_run[nc];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) out[e] = (bf16_t)(r[e] * inv);
-                    *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * kg) = out;
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        const float* pc = piece_of(min(j + k * WAVES, w1));   // past the end: the last one, with weight 0
+                        x[k] = get(pc + COLS * D_H + nc * 32 + c * 2);
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            v[k][dt][0] = get(pc + (dt * NC + nc) * 256 + ln * 2);
+                            v[k][dt][1] = get(pc + (dt * NC + nc) * 256 + 128 + ln * 2);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) m = fmaxf(m, j + k * WAVES <= w1 ? x[k].x : -INFINITY);
+                    const float ref = m == -INFINITY ? 0.0f : m, keep = __builtin_amdgcn_exp2f(m_run[nc] - ref);
+                    l_run[nc] *= keep;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) acc[dt][nc] *= keep;
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        const float f = j + k * WAVES <= w1 ? __builtin_amdgcn_exp2f(x[k].x - ref) : 0.0f;
+                        if (quad == 0) l_run[nc] += x[k].y * f;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) acc[dt][nc] += f * f32x4{v[k][dt][0].x, v[k][dt][0].y, v[k][dt][1].x, v[k][dt][1].y};
+                    }
+                    m_run[nc] = m;
                 }
             }
-            if (!whole && w == 0 && kg == 0) put(piece + COLS * D_H + (nc * 16 + c16) * 2, m, l);
-        }
-        if (whole) {
-            __syncthreads();                               // the rings are free again
-            continue;
-        }
-        // ---- a cut block: the workgroup that comes last adds the pieces, in the order of their keys ----
-        const int w0 = (int)((u0 + START) / per), w1 = (int)((u1 - 1) / per);
-        wait_loads<0>();                                   // the piece is written
-        __syncthreads();
-        if (tid == 0) {
-            const int before = __hip_atomic_fetch_add(&a.arrived[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last_here = before == w1 - w0;
-            if (last_here) __hip_atomic_store(&a.arrived[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (!last_here) continue;
-        for (int e = tid; e < DT * NC * 64; e += 64 * WAVES) {
-            const int ln = e & 63, dn = e >> 6, nc = dn % NC, dt = dn / NC;
-            const int cc = nc * 16 + (ln & 15), col = blk * COLS + cc, i = col / a.g, hg = col - i * a.g;
-            if (i >= n_new) continue;
-            float m = -INFINITY, l = 0.0f;
-            f32x4 r = {0.f, 0.f, 0.f, 0.f};
-            for (int j = w0; j <= w1; ++j) {
-                const float* pc = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * COLS * (D_H + 2);
-                const float2 x = get(pc + COLS * D_H + cc * 2), va = get(pc + (dn * 128 + ln) * 2), vb = get(pc + (dn * 128 + 64 + ln) * 2);
-                const f32x4 v = {va.x, va.y, vb.x, vb.y};
-                const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.0f : mn;
-                const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(x.x - ref);
-                l = l * keep + x.y * f;
-                r = r * keep + v * f;
-                m = mn;
-            }
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            bf16x4 out;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) out[k] = (bf16_t)(r[k] * inv);
-            *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(row0 + i) * a.H_q + h * a.g + hg) * D_H + dt * 16 + 4 * (ln >> 4)) = out;
         }
     }
 }
@@ -658,22 +675,16 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
                     (float*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn, ws.arrived};
     const int grid = std::min(cc_device_cus(), CC_PAGED_WGS);
     const int64_t columns = (int64_t)std::min(r.max_new, r.rows) * g;
-    const int per_min = 2 * WAVES + START;
-    if (columns > 64) {
+    const int per_min = WAVES + START;                     // a tile for each wave
+    if (!cc_few_rows(columns, m.d_h)) {
         const int chunk_min = 3 + CHUNK_START;
         if (m.d_h == 128) hipLaunchKernelGGL(chunk_attn_kernel<128>, dim3(grid), dim3(512), 0, s, a, chunk_min);
         else hipLaunchKernelGGL(chunk_attn_kernel<64>, dim3(grid), dim3(512), 0, s, a, chunk_min);
         return;
     }
 #define CC_FEW(D, NC) hipLaunchKernelGGL((few_attn_kernel<D, NC>), dim3(grid), dim3(64 * WAVES), 0, s, a, per_min)
-    if (m.d_h == 128) {
-        if (columns <= 16) CC_FEW(128, 1);
-        else if (columns <= 32) CC_FEW(128, 2);
-        else CC_FEW(128, 4);
-    } else {
-        if (columns <= 16) CC_FEW(64, 1);
-        else if (columns <= 32) CC_FEW(64, 2);
-        else CC_FEW(64, 4);
-    }
+    if (m.d_h == 128) CC_FEW(128, 1);
+    else if (columns <= 16) CC_FEW(64, 1);
+    else CC_FEW(64, 2);
 #undef CC_FEW
 }

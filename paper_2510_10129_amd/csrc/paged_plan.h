@@ -34,6 +34,12 @@ inline cc_page_work cc_page_work_layout(int64_t n_pages, int64_t n_seqs) {
     return w;
 }
 
+// Which attention kernel takes a batch whose sequences have up to so many (row, query head of a group) columns: few rows read
+// every key once per 16 columns (32 at d_h = 64) from a ring a wave, many rows multiply 256 columns a workgroup.  16 sequences of 4000
+// to 12000 tokens, us few / many:  d_h = 128, 32 heads of 8, 4 columns 100 / 121, 16 columns 97 / 110, 20 columns (two blocks of 16 a
+// wave) 147 / 115;  d_h = 64, 32 of 8, 4 columns 61 / 79, 32 columns 66 / 79, 64 columns (four blocks) 114 / 88.
+inline bool cc_few_rows(int64_t columns, int32_t d_h) { return columns <= (d_h == 128 ? 16 : 32); }
+
 struct cc_refusal {
     cc_status code;
     const char* why;
@@ -52,8 +58,8 @@ inline cc_refusal cc_check_pool(const cc_page_pool* p) {
                  "page_size must be a power of two in [16, 1024]");
     CC_REFUSE_IF(p->n_pages < 1 || p->n_seqs < 1 || p->n_seqs > 65536 || p->max_pages < 1, CC_ERR_SHAPE,
                  "need n_pages >= 1, max_pages >= 1 and n_seqs in [1, 65536]");
-    CC_REFUSE_IF((int64_t)p->n_pages * p->page_size >= (1ll << 31) || (int64_t)p->max_pages * p->page_size >= (1ll << 31),
-                 CC_ERR_SHAPE, "n_pages * page_size and max_pages * page_size must be below 2^31");
+    CC_REFUSE_IF((int64_t)p->n_pages * p->page_size >= (1ll << 31) || (int64_t)p->max_pages * p->page_size >= (1ll << 30),
+                 CC_ERR_SHAPE, "n_pages * page_size must be below 2^31, max_pages * page_size below 2^30");
     CC_REFUSE_IF(p->stride_table < p->max_pages, CC_ERR_SHAPE, "stride_table must be at least max_pages");
     CC_REFUSE_IF(!cc_aligned(p->refs, 4) || !cc_aligned(p->table, 4) || !cc_aligned(p->len, 4) || !cc_aligned(p->status, 4) ||
                      !cc_aligned(p->work, 256), CC_ERR_SHAPE, "tables must be 4-byte aligned and work 256-byte aligned");
@@ -74,7 +80,7 @@ inline cc_refusal cc_check_paged_kv(const cc_paged_kv* kv, int32_t page_size, in
     CC_REFUSE_IF(H_kv > 1 && !tokens_out && !heads_out, CC_ERR_SHAPE, "tokens or heads must be outermost in a page");
     CC_REFUSE_IF(kv->stride_page < (page_size - 1) * kv->stride_token + (H_kv - 1) * kv->stride_head + d_h, CC_ERR_SHAPE,
                  "stride_page must cover a page");
-    CC_REFUSE_IF(kv->stride_token >= (1ll << 24), CC_ERR_SHAPE, "stride_token must be below 2^24");
+    CC_REFUSE_IF(kv->stride_token >= (1ll << 23), CC_ERR_SHAPE, "stride_token must be below 2^23");
     CC_REFUSE_IF(!cc_aligned(kv->K, 16) || !cc_aligned(kv->V, 16), CC_ERR_SHAPE, "K and V must be 16-byte aligned");
     return {CC_OK, ""};
 }

@@ -10,6 +10,7 @@
 namespace {
 
 constexpr int NT = 1024;
+constexpr int ROWS = 8;                      // entries of a table row that a lane loads before it stores the first
 
 // Inclusive scan over the workgroup; every thread comes here.  part: NT / 64 entries of LDS.
 template <class T>
@@ -142,32 +143,51 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
     finish(status, host, 0);
 }
 
+// A source that is listed many times is counted first: its pages' counts are raised once, by the entry that was the first to
+// count it (eight answers from each of four contexts: 13.3 us with every entry adding for itself).
 __global__ __launch_bounds__(NT) void fork_kernel(cc_pool_view p, const int32_t* __restrict__ src,
                                                   const int32_t* __restrict__ dst, int n, int32_t* work, cc_page_work w,
                                                   int32_t* status, int32_t* host) {
     __shared__ int bad;
     const int tid = threadIdx.x, page = 1 << p.shift;
+    int32_t *taken = work + w.mark, *copies = work + w.first, *len = work + w.take, *leads = work + w.copy_at;
     if (tid == 0) bad = 0;
     __syncthreads();
-    check_distinct(dst, n, p.n_seqs, work + w.mark, &bad);
     for (int i = tid; i < n; i += NT) {
         const int s = src[i], d = dst[i];
-        if ((unsigned)s >= (unsigned)p.n_seqs || ((unsigned)d < (unsigned)p.n_seqs && p.len[d] != 0)) atomicOr(&bad, BAD_INDEX);
-        else work[w.take + i] = cc_seq_len(p, s);             // as it is at the call
+        if ((unsigned)s >= (unsigned)p.n_seqs || (unsigned)d >= (unsigned)p.n_seqs || p.len[d] != 0) {
+            atomicOr(&bad, BAD_INDEX);
+        } else {
+            taken[d] = 0;
+            copies[s] = 0;
+            len[i] = cc_seq_len(p, s);                        // as it is at the call
+        }
+    }
+    __syncthreads();
+    if (bad) return finish(status, host, bad);
+    for (int i = tid; i < n; i += NT) {
+        if (atomicAdd(&taken[dst[i]], 1)) atomicOr(&bad, BAD_INDEX);
+        leads[i] = atomicAdd(&copies[src[i]], 1) == 0;
     }
     __syncthreads();
     if (bad) return finish(status, host, bad);
     const int lane = tid & 63;
     for (int i = tid >> 6; i < n; i += NT / 64) {
-        const int L = work[w.take + i], held = (L + page - 1) >> p.shift;
-        const int32_t* from = p.table + src[i] * p.st_table;
-        int32_t* to = p.table + dst[i] * p.st_table;
-        for (int c = lane; c < held; c += 64) {
-            const int q = from[c];
-            to[c] = q;
-            if ((unsigned)q < (unsigned)p.n_pages) atomicAdd(&p.refs[q], 1);
+        const int s = src[i], d = dst[i], L = len[i], held = (L + page - 1) >> p.shift, more = leads[i] ? copies[s] : 0;
+        const int32_t* from = p.table + s * p.st_table;
+        int32_t* to = p.table + d * p.st_table;
+        for (int c0 = lane; c0 < held; c0 += 64 * ROWS) {
+            int q[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) q[k] = from[min(c0 + 64 * k, held - 1)];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                if (c0 + 64 * k >= held) break;
+                to[c0 + 64 * k] = q[k];
+                if (more && (unsigned)q[k] < (unsigned)p.n_pages) atomicAdd(&p.refs[q[k]], more);
+            }
         }
-        if (lane == 0) p.len[dst[i]] = L;
+        if (lane == 0) p.len[d] = L;
     }
     finish(status, host, 0);
 }
@@ -184,10 +204,16 @@ __global__ __launch_bounds__(NT) void free_kernel(cc_pool_view p, const int32_t*
     for (int i = tid >> 6; i < n; i += NT / 64) {
         const int s = seq[i], held = (cc_seq_len(p, s) + page - 1) >> p.shift;
         int32_t* row = p.table + s * p.st_table;
-        for (int c = lane; c < held; c += 64) {
-            const int q = row[c];
-            row[c] = -1;
-            if ((unsigned)q < (unsigned)p.n_pages) atomicSub(&p.refs[q], 1);
+        for (int c0 = lane; c0 < held; c0 += 64 * ROWS) {
+            int q[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) q[k] = row[min(c0 + 64 * k, held - 1)];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                if (c0 + 64 * k >= held) break;
+                row[c0 + 64 * k] = -1;
+                if ((unsigned)q[k] < (unsigned)p.n_pages) atomicSub(&p.refs[q[k]], 1);
+            }
         }
         if (lane == 0) p.len[s] = 0;
     }
@@ -254,11 +280,15 @@ struct copy_args {
     void* ptr[2 * CC_PAGE_LAYERS];
     int32_t n_ptr;
 };
-// A workgroup takes a (copy, tensor) at a time: the copy's rows of all heads, 16 bytes a lane.
+// A workgroup takes a (copy, tensor) at a time: the copy's rows of all heads, eight pieces of 16 bytes a thread loaded before
+// the first is stored, all past the caches.  Bound by HBM.
 template <int D_H>
 __global__ __launch_bounds__(256) void page_copy_kernel(copy_args a, const int32_t* __restrict__ work, cc_page_work w,
-                                                        int H_kv, int64_t st_page, int64_t st_tok, int64_t st_head) {
-    constexpr int CPH = D_H / 8;
+                                                        int H_kv, int page, int64_t st_page, int64_t st_tok, int64_t st_head) {
+    constexpr int CPH = D_H / 8, NB = 8;
+    const bool by_token = st_tok > st_head || H_kv == 1;
+    const bool gapless = by_token ? st_tok == (int64_t)H_kv * D_H && (H_kv == 1 || st_head == D_H)
+                                  : st_head == (int64_t)page * D_H && st_tok == D_H;
     const int64_t items = (int64_t)work[0] * a.n_ptr;
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
         const int i = (int)(it / a.n_ptr), t = (int)(it - (int64_t)i * a.n_ptr);
@@ -266,11 +296,24 @@ __global__ __launch_bounds__(256) void page_copy_kernel(copy_args a, const int32
         bf16_t* base = (bf16_t*)a.ptr[t];
         const bf16_t* from = base + work[w.src + i] * st_page;
         bf16_t* to = base + work[w.dst + i] * st_page;
-        for (int u = threadIdx.x; u < units; u += 256) {
+        const bool flat = gapless && (by_token || rows == page);
+        auto place = [&](int u) -> int64_t {
+            if (flat) return (int64_t)u * 8;
             const int c = u % CPH, r = u / CPH;
-            const int tok = st_tok > st_head ? r / H_kv : r % rows, h = st_tok > st_head ? r % H_kv : r / rows;
-            const int64_t at = tok * st_tok + h * st_head + c * 8;
-            *reinterpret_cast<u32x4*>(to + at) = *reinterpret_cast<const u32x4*>(from + at);
+            const int tok = by_token ? r / H_kv : r % rows, h = by_token ? r % H_kv : r / rows;
+            return tok * st_tok + h * st_head + c * 8;
+        };
+        for (int u0 = threadIdx.x; u0 < units; u0 += 256 * NB) {
+            u32x4 x[NB];
+            int64_t at[NB];
+#pragma unroll
+            for (int k = 0; k < NB; ++k) {
+                at[k] = place(min(u0 + k * 256, units - 1));
+                x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + at[k]));
+            }
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+                if (u0 + k * 256 < units) __builtin_nontemporal_store(x[k], reinterpret_cast<u32x4*>(to + at[k]));
         }
     }
 }
@@ -441,13 +484,15 @@ void cc_launch_page_copies(const cc_page_pool& p, const cc_paged_kv* kv, int n_l
         copy_args a;
         a.n_ptr = 2 * std::min(CC_PAGE_LAYERS, n_layers - l0);
         for (int i = 0; i < a.n_ptr; ++i) a.ptr[i] = i & 1 ? kv[l0 + i / 2].V : kv[l0 + i / 2].K;
-        const dim3 grid((unsigned)std::min<int64_t>((int64_t)most * a.n_ptr, 8 * cc_device_cus()));
+        const dim3 grid((unsigned)std::min<int64_t>((int64_t)most * a.n_ptr, 64 * cc_device_cus()));
         if (grid.x == 0) return;
         if (d_h == 128)
-            hipLaunchKernelGGL(page_copy_kernel<128>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, kv[0].stride_page,
+            hipLaunchKernelGGL(page_copy_kernel<128>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, p.page_size,
+                               kv[0].stride_page,
                                kv[0].stride_token, kv[0].stride_head);
         else
-            hipLaunchKernelGGL(page_copy_kernel<64>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, kv[0].stride_page,
+            hipLaunchKernelGGL(page_copy_kernel<64>, grid, dim3(256), 0, s, a, (const int32_t*)p.work, w, H_kv, p.page_size,
+                               kv[0].stride_page,
                                kv[0].stride_token, kv[0].stride_head);
     }
 }

@@ -66,12 +66,12 @@ def test_pool_checks(lib):
         assert lib.pool(C.byref(_pool(**{name: None}))) == CC_ERR_NULL
     for bad in (dict(page_size=8), dict(page_size=24), dict(page_size=2048), dict(n_pages=0), dict(n_seqs=0), dict(n_seqs=65537),
                 dict(max_pages=0), dict(stride_table=7), dict(work=A + 64), dict(table=A + 2), dict(n_pages=1 << 27),
-                dict(max_pages=1 << 27, stride_table=1 << 27), dict(n_pages=-1), dict(page_size=-16)):
+                dict(max_pages=1 << 26, stride_table=1 << 26), dict(n_pages=-1), dict(page_size=-16)):
         assert lib.pool(C.byref(_pool(**bad))) == CC_ERR_SHAPE, bad
     need = lib.work(64, 4)
     assert need == _lib.load_library().cc_page_work_bytes(64, 4) > 0
     assert lib.pool(C.byref(_pool(work_bytes=need - 1))) == CC_ERR_WORKSPACE and lib.pool(C.byref(_pool(work_bytes=need))) == CC_OK
-    assert lib.pool(C.byref(_pool(page_size=1024, n_pages=(1 << 21) - 1, max_pages=(1 << 21) - 1, stride_table=1 << 21))) == CC_OK
+    assert lib.pool(C.byref(_pool(page_size=1024, n_pages=(1 << 21) - 1, max_pages=(1 << 20) - 1, stride_table=1 << 20))) == CC_OK
     assert _lib.load_library().cc_page_work_bytes(0, 4) == 0
 
 
@@ -101,7 +101,7 @@ def test_layer_checks(lib):
     assert code(kv(K=None)) == CC_ERR_NULL and lib.layers(None, 1, 16, 4, 128) == CC_ERR_NULL
     for bad in (dict(stride_page=16 * 4 * 128 - 8), dict(stride_token=4 * 128 + 4), dict(stride_head=120), dict(stride_token=64),
                 dict(stride_head=256), dict(K=A + 8), dict(V=A + 2), dict(stride_page=0), dict(stride_page=-8),
-                dict(stride_token=1 << 24, stride_page=1 << 29)):
+                dict(stride_token=1 << 23, stride_page=1 << 28)):
         assert code(kv(**bad)) == CC_ERR_SHAPE, bad
     assert code(kv(), kv(stride_page=1 << 20)) == CC_ERR_SHAPE and lib.layers(None, -1, 16, 4, 128) == CC_ERR_SHAPE
 
