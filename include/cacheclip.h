@@ -294,7 +294,7 @@ int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs);
 
 /* One layer's pages, dev bf16: element (page, token, head, c) of K and V is at
  * page*stride_page + token*stride_token + head*stride_head + c (elements; strides multiples of 8, c contiguous,
- * tokens or heads outermost in a page, stride_token < 2^23).  Slots behind a sequence's last token may hold anything; the others must be
+ * tokens or heads outermost in a page, stride_token < 2^23, page_size * stride_token < 2^31).  Slots behind a sequence's last token may hold anything; the others must be
  * finite, as everywhere in this library.  A page outside [0, n_pages) reads as zeros and is never written, so that
  * pages which slid out of every window may be given back. */
 typedef struct cc_paged_kv {

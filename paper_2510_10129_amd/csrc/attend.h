@@ -88,7 +88,7 @@ __device__ __forceinline__ int last_key(const int32_t* idx, int M, int g, int rt
 
 // Keys and values in one cache: row i of the recomputed rows sees every slot up to idx[i].
 struct one_cache {
-    static constexpr bool paged = false;
+    static constexpr bool paged = false, wide_pages = true;
     const int32_t* idx;
     const bf16_t* K;
     const bf16_t* V;
@@ -99,6 +99,12 @@ struct one_cache {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t uniform(int64_t v) {
     return ((int64_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
+}
+
+// The value, where it is asked for: what is made of it is not made ahead and kept through code in front of it.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
 // Eight bytes of a piece, past the L2 and read past it: pieces go from one XCD to another within a launch.  A fence over the whole
@@ -135,10 +141,12 @@ __device__ __forceinline__ tile_span visible_tiles(int first, int end, int windo
 
 // Keys and values in pages: row i of a sequence's new rows sits at position first + i.  The visible key tiles of a
 // row tile are `span`'s; within them a row sees key j up to its position, if it is within its window or a sink.
+// WIDE_PAGES: pages of 64 tokens and more, so that a tile lies in one; else every 16 keys have a page of their own.
+typedef const __attribute__((address_space(4))) int32_t* scalar_table;   // constant for the launch: scalar loads
+template <bool WIDE_PAGES>
 struct in_pages {
-    static constexpr bool paged = true;
-    typedef const __attribute__((address_space(4))) int32_t* table_t;   // constant for the launch: scalar loads
-    table_t table;                  // of the sequence
+    static constexpr bool paged = true, wide_pages = WIDE_PAGES;
+    scalar_table table;             // of the sequence
     const bf16_t* K;
     const bf16_t* V;
     const bf16_t* zeros;            // a row of them, for what no page holds
@@ -166,7 +174,7 @@ __device__ __forceinline__ void attend(
     auto k_stage = [&](int t) __attribute__((always_inline)) { return smem + (t % 3) * TILE; };
     auto v_stage = [&](int t) __attribute__((always_inline)) { return smem + (3 + t % 4) * TILE; };
 
-    const int lane = threadIdx.x & 63;
+    const int lane = Keys::paged ? here(threadIdx.x & 63) : threadIdx.x & 63;
     const int wave = widx;                              // role in the cooperative tile loads
     const int qr = lane & 31, hf = lane >> 5;
     const int col_in = (grp * 4 + widx) * 32 + qr;      // column within the row tile
@@ -241,24 +249,29 @@ __device__ __forceinline__ void attend(
         const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
         return reinterpret_cast<const char*>((hi << 32) | lo);
     };
-    // In pages every instruction has a base of its own: its rows (4 or 8, aligned) lie in one page.  The pages of a tile
-    // are asked for a tile ahead.  Rows behind the last token repeat it (only the last tile's can be); a group of
-    // rows that no page holds is read from the zeros.
+    // In pages a tile has one base, or every instruction one of its own: its rows (4 or 8, aligned) lie in one page.  The
+    // pages of a tile are asked for a tile ahead.  Rows behind the last token repeat it (only the last tile's can be); what
+    // no page holds is read from a row of zeros.
+    constexpr int NB = Keys::wide_pages ? 1 : NI;      // bases of a tile
     Off loff[NI];
-    struct tile_src { const char* at[Keys::paged ? NI : 1]; };
-    int next_page[Keys::paged ? NI : 1];
+    struct tile_src { const char* at[NB]; bool there[NB]; };
+    int next_page[NB];
+    // first key of the 16 that instruction i takes its rows of, and its first row within them (narrow pages)
+    auto group = [&](int i) __attribute__((always_inline)) -> int { return (i * 4 + wave) * RPI & ~15; };
+    const int group_row = wave * RPI & 15;
     auto ask_pages = [&](int t) __attribute__((always_inline)) {
         if constexpr (Keys::paged) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i)
-                next_page[i] = keys.table[min(key_of(t) + (i * 4 + wave) * RPI, max(keys.L - 1, 0)) >> keys.shift];
+            for (int i = 0; i < NB; ++i)
+                next_page[i] = keys.table[min(key_of(t) + (NB == 1 ? 0 : group(i)), max(keys.L - 1, 0)) >> keys.shift];
         }
     };
     auto set_loff = [&](int rmax) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            if constexpr (Keys::paged) loff[i] = ((Off)max(min(l_row, rmax - (i * 4 + wave) * RPI), 0) * (Off)keys.st_tok + (Off)l_col) * 2;
-            else loff[i] = ((Off)min(r0 + i * 4 * RPI, rmax) * (Off)keys.st + (Off)l_col) * 2;
+            if constexpr (!Keys::paged) loff[i] = ((Off)min(r0 + i * 4 * RPI, rmax) * (Off)keys.st + (Off)l_col) * 2;
+            else if constexpr (NB == 1) loff[i] = ((Off)max(min(r0 + i * 4 * RPI, rmax), 0) * (Off)keys.st_tok + (Off)l_col) * 2;
+            else loff[i] = ((Off)max(min(group_row + l_row, rmax - group(i)), 0) * (Off)keys.st_tok + (Off)l_col) * 2;
         }
     };
     set_loff(BN_KEYS);
@@ -268,11 +281,12 @@ __device__ __forceinline__ void attend(
         if constexpr (Keys::paged) {
             if (j0 + BN_KEYS > keys.L) set_loff(keys.L - 1 - j0);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int key = j0 + (i * 4 + wave) * RPI;
-                const bool there = key < keys.L && (unsigned)next_page[i] < (unsigned)keys.n_pages;
-                src.at[i] = there ? lbase + (next_page[i] * keys.st_page + (int64_t)(key & ((1 << keys.shift) - 1)) * keys.st_tok) * 2
-                                  : nullptr;
+            for (int i = 0; i < NB; ++i) {
+                const int key = j0 + (NB == 1 ? 0 : group(i));
+                src.there[i] = key < keys.L && (unsigned)next_page[i] < (unsigned)keys.n_pages;
+                // (a page is smaller than 2^32 bytes)
+                src.at[i] = lbase + (next_page[i] * keys.st_page * 2 + (uint32_t)(key & ((1 << keys.shift) - 1)) * (uint32_t)(keys.st_tok * 2));
+                if (!src.there[i]) src.at[i] = (const char*)keys.zeros;
             }
         } else {
             if (j0 + BN_KEYS > keys.N) set_loff(keys.N - 1 - j0);
@@ -282,14 +296,12 @@ __device__ __forceinline__ void attend(
     };
     auto load_part = [&](const tile_src& tile, bf16_t* stage, auto ic) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value;
+        const char* b = scalar_ptr(tile.at[NB == 1 ? 0 : i] - i * 1024);   // the immediate adds it back
         if constexpr (Keys::paged) {
-            const bool there = tile.at[i] != nullptr;
-            const char* b = scalar_ptr((there ? tile.at[i] : (const char*)keys.zeros) - i * 1024);
-            Off off = there ? loff[i] : (Off)(l_col * 2);
+            Off off = tile.there[NB == 1 ? 0 : i] ? loff[i] : (Off)(l_col * 2);
             asm volatile("" : "+v"(off));
             dma16<i * 1024>(reinterpret_cast<const bf16_t*>(b + off), stage + wave_slot);
         } else {
-            const char* b = scalar_ptr(tile.at[0] - i * 1024);           // the immediate adds it back
             asm volatile("" : "+v"(loff[i]));   // keeps the (32-bit) offset a register operand of the load
             dma16<i * 1024>(reinterpret_cast<const bf16_t*>(b + loff[i]), stage + wave_slot);
         }

@@ -27,6 +27,8 @@ constexpr int START = 4;                      // units that a block costs beside
 // Blocks of up to so many tiles are not cut where every block can have a workgroup: 512 tokens take 8.3 us either way, 256
 // take 6.2 whole and 7.3 in pieces (one sequence, 4 query heads of 2, d_h 64), 7.0 and 8.6 (32 of 8, d_h 128).
 constexpr int WHOLE = 16;
+// Longer ones are cut at multiples of the shortest range from their start on, if there are workgroups for it: one with the end
+// of a block and the start of another takes 3 us more (8 sequences of 1073 tokens, 4 heads of 2: 13.0 us in equal ranges, 10.4 so).
 
 // 16 bytes per lane from global memory into LDS at wave base + OFF + 16 * lane; OFF is added to the global address too.
 // Non-temporal: what few rows read is read once.
@@ -74,11 +76,6 @@ __device__ __forceinline__ batch_seq seq_of(const paged_args& a, int b) {
     return r;
 }
 
-// The value, where it is asked for: what is made of it is not made ahead and kept through the loop in front of it.
-__device__ __forceinline__ int here(int v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
 __device__ __forceinline__ int64_t of_lane(int64_t v, int l) {
     return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, l);
 }
@@ -125,7 +122,8 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
     const bool small = a.n <= 64;
     batch_seq mine = {0, 0, 0, 0};
     int64_t my_end = 0, my_units = 0, total;
-    int whole_len = 0;        // > 0: no block is cut, and each is as long as the longest
+    // > 0: no workgroup has two blocks: every block starts a range of so many units and is as long as whole ranges
+    int aligned = 0;
     if (small) {
         mine = seq_of(a, min(lane, a.n - 1));
         if (lane >= a.n) mine.n = 0;
@@ -135,7 +133,12 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             blocks += __shfl_xor(blocks, off);
         }
         longest = uniform(longest);
-        if (longest <= WHOLE + START && uniform(blocks) <= (int)gridDim.x) whole_len = len = longest;
+        blocks = uniform(blocks);
+        if (blocks > 0 && blocks <= (int)gridDim.x) {
+            if (longest <= WHOLE + START) aligned = longest;
+            else if ((longest + per_min - 1) / per_min <= (int)gridDim.x / blocks) aligned = per_min;
+        }
+        if (aligned > 0) len = (len + aligned - 1) / aligned * aligned;
         my_units = (int64_t)blocks_of(mine) * len;
         my_end = wave_scan(my_units, a.n);
         total = of_lane(my_end, a.n - 1);
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         __syncthreads();
         total = uniform(pre[a.n]);
     }
-    const int64_t per = whole_len > 0 ? whole_len : max((int64_t)per_min, quotient(total + gridDim.x - 1, gridDim.x));
+    const int64_t per = aligned > 0 ? aligned : max((int64_t)per_min, quotient(total + gridDim.x - 1, gridDim.x));
     const int range = blockIdx.x;
     int64_t u = range * per;
     const int64_t stop = min(u + per, total);
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         }
         const int first = L - n_new;
         const tile_span span = visible_tiles(first, L, a.window, a.sinks, KEYS);
-        const int len = whole_len > 0 ? whole_len : span.count + START;
+        const int real = span.count + START, len = aligned > 0 ? (real + aligned - 1) / aligned * aligned : real;
         const int which = (int)quotient(u - seq0, len), blk = which / a.H_kv, h = which - blk * a.H_kv;
         const int64_t u0 = seq0 + (int64_t)which * len, u1 = u0 + len;
         const int ta = (int)max((int64_t)0, u - u0 - START), te = min((int)(min(u1, stop) - u0) - START, span.count);
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         const int nt = te - ta > w ? (te - ta - w + WAVES - 1) / WAVES : 0;
         auto tile_key = [&](int k) { return span.tile(ta + w + k * WAVES) * KEYS; };
         // (scalar loads do not count among the loads that the waits below count)
-        const in_pages::table_t row_table = (in_pages::table_t)(a.p.table + s * a.p.st_table);
+        const scalar_table row_table = (scalar_table)(a.p.table + s * a.p.st_table);
         const int64_t head_off = (int64_t)h * a.st_head;
         // The two pages of a tile (16 keys each, in one page): those of the first NS tiles together, the others' a tile ahead.
         struct pages { int a, b; };
@@ -455,7 +458,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
         // ---- A cut block: a range leaves at most two pieces, of the block it starts in and of a later one.  The workgroup
         // that comes last adds them: a wave takes every fourth, then as above.  (Stores past the L2 have been
         // acknowledged before the count is raised, and loads past it follow the count: no fence is needed.) ----
-        const int w0 = (int)quotient(u0 + START, per), w1 = (int)quotient(u1 - 1, per);
+        const int w0 = (int)quotient(u0 + START, per), w1 = (int)quotient(u0 + real - 1, per);
         auto piece_of = [&](int j) { return a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * COLS * (D_H + 2); };
         wait_loads<0>();
         float* piece = ta == 0 && te == span.count ? nullptr : piece_of(range);
@@ -519,7 +522,7 @@ constexpr int MAX_BLOCKS = CC_PAGED_MAX_COLUMNS / 256 + CC_PAGED_MAX_N;
 
 // A workgroup of eight waves per range.  Blocks are numbered e0(b) + row tile with e0(b) = floor(columns in front of b / 256) + b:
 // at least as many numbers as sequence b has row tiles, the unused ones of length 0, and no scan is needed to find one.
-template <int D_H>
+template <int D_H, bool WIDE_PAGES>
 __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int per_min) {
     __shared__ __align__(16) bf16_t smem[LDS_TILES * BN_KEYS * D_H];
     __shared__ int simd_waves[4], group_waves[2], wave_units[8], last_here;
@@ -603,8 +606,8 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         const int64_t u0 = (int64_t)kvh * head_units + b0;
         u = u0 + len;
         if (te <= ta) continue;
-        in_pages keys;
-        keys.table = (in_pages::table_t)(a.p.table + uniform(sq.s) * a.p.st_table);
+        in_pages<WIDE_PAGES> keys;
+        keys.table = (scalar_table)(a.p.table + uniform(sq.s) * a.p.st_table);
         keys.K = a.K, keys.V = a.V, keys.zeros = a.zeros;
         keys.st_page = a.st_page, keys.st_tok = a.st_tok, keys.sh = a.st_head;
         keys.shift = a.p.shift, keys.n_pages = a.p.n_pages, keys.L = L, keys.first = first, keys.row0 = uniform(sq.row0);
@@ -626,29 +629,49 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         }
         __syncthreads();
         if (!last_here) continue;
-        // a thread holds what the lane that left it did: half of a column's sums
-        constexpr int NG = D_H / 8;
+        // A thread holds what the lane that left it did: half of a column's sums, in two passes; up to four
+        // pieces are asked for together (one after the other they took 1.9 us each).
+        constexpr int NG = D_H / 16;
         const int col = rt * 256 + w * 32 + (lane & 31), mi = col / a.g, hg = col - mi * a.g;
-        if (mi < n_new) {
+        if (mi >= n_new) continue;
+        for (int k0 = 0; k0 < D_H / 8; k0 += NG) {
             f32x4 acc[NG];
             float m = -INFINITY, l = 0.0f;
 #pragma unroll
             for (int k = 0; k < NG; ++k) acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int j = w0; j <= w1; ++j) {
-                const float* pp = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * 256 * (D_H + 4) + w * 32 * (D_H + 4);
-                const float2 ml = get(pp + 32 * D_H + lane * 2);
-                float2 v[NG][2];
+            auto take = [&](auto nc, int j0) __attribute__((always_inline)) {
+                constexpr int NP = decltype(nc)::value;
+                float2 ml[NP], v[NP][NG][2];
 #pragma unroll
-                for (int k = 0; k < NG; ++k) {
-                    v[k][0] = get(pp + k * 256 + lane * 2);
-                    v[k][1] = get(pp + k * 256 + 128 + lane * 2);
+                for (int i = 0; i < NP; ++i) {
+                    const int j = min(j0 + i, w1);         // past the end: the last piece again, with weight 0
+                    const float* pp = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * 256 * (D_H + 4) + w * 32 * (D_H + 4);
+                    ml[i] = get(pp + 32 * D_H + lane * 2);
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        v[i][k][0] = get(pp + (k0 + k) * 256 + lane * 2);
+                        v[i][k][1] = get(pp + (k0 + k) * 256 + 128 + lane * 2);
+                    }
                 }
-                const float mn = fmaxf(m, ml.x), ref = mn == -INFINITY ? 0.0f : mn;
-                const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
-                l = l * keep + ml.y * f;
+                float mn = m;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) mn = fmaxf(mn, ml[i].x);
+                const float ref = mn == -INFINITY ? 0.0f : mn, keep = __builtin_amdgcn_exp2f(m - ref);
+                l *= keep;
                 m = mn;
 #pragma unroll
-                for (int k = 0; k < NG; ++k) acc[k] = acc[k] * keep + f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y} * f;
+                for (int k = 0; k < NG; ++k) acc[k] *= keep;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const float f = j0 + i <= w1 ? __builtin_amdgcn_exp2f(ml[i].x - ref) : 0.0f;
+                    l += ml[i].y * f;
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) acc[k] += f * f32x4{v[i][k][0].x, v[i][k][0].y, v[i][k][1].x, v[i][k][1].y};
+                }
+            };
+            for (int j = w0; j <= w1;) {
+                if (w1 - j >= 2) take(std::integral_constant<int, 4>{}, j), j += 4;
+                else take(std::integral_constant<int, 2>{}, j), j += 2;
             }
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
             bf16_t* op = a.o + ((int64_t)(keys.row0 + mi) * a.H_q + kvh * a.g + hg) * D_H + 4 * (lane >> 5);
@@ -657,7 +680,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
                 bf16x4 r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r[i] = (bf16_t)(acc[k][i] * inv);
-                *reinterpret_cast<bf16x4*>(op + 8 * k) = r;
+                *reinterpret_cast<bf16x4*>(op + 8 * (k0 + k)) = r;
             }
         }
     }
@@ -678,8 +701,16 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
     const int per_min = WAVES + START;                     // a tile for each wave
     if (!cc_few_rows(columns, m.d_h)) {
         const int chunk_min = 3 + CHUNK_START;
-        if (m.d_h == 128) hipLaunchKernelGGL(chunk_attn_kernel<128>, dim3(grid), dim3(512), 0, s, a, chunk_min);
-        else hipLaunchKernelGGL(chunk_attn_kernel<64>, dim3(grid), dim3(512), 0, s, a, chunk_min);
+#define CC_CHUNK(D, WIDE) hipLaunchKernelGGL((chunk_attn_kernel<D, WIDE>), dim3(grid), dim3(512), 0, s, a, chunk_min)
+        const bool wide = p.page_size >= BN_KEYS;          // a tile of keys lies in one page
+        if (m.d_h == 128) {
+            if (wide) CC_CHUNK(128, true);
+            else CC_CHUNK(128, false);
+        } else {
+            if (wide) CC_CHUNK(64, true);
+            else CC_CHUNK(64, false);
+        }
+#undef CC_CHUNK
         return;
     }
 #define CC_FEW(D, NC) hipLaunchKernelGGL((few_attn_kernel<D, NC>), dim3(grid), dim3(64 * WAVES), 0, s, a, per_min)

@@ -80,7 +80,8 @@ inline cc_refusal cc_check_paged_kv(const cc_paged_kv* kv, int32_t page_size, in
     CC_REFUSE_IF(H_kv > 1 && !tokens_out && !heads_out, CC_ERR_SHAPE, "tokens or heads must be outermost in a page");
     CC_REFUSE_IF(kv->stride_page < (page_size - 1) * kv->stride_token + (H_kv - 1) * kv->stride_head + d_h, CC_ERR_SHAPE,
                  "stride_page must cover a page");
-    CC_REFUSE_IF(kv->stride_token >= (1ll << 23), CC_ERR_SHAPE, "stride_token must be below 2^23");
+    CC_REFUSE_IF(kv->stride_token >= (1ll << 23) || kv->stride_token * page_size >= (1ll << 31), CC_ERR_SHAPE,
+                 "stride_token must be below 2^23, and times page_size below 2^31");
     CC_REFUSE_IF(!cc_aligned(kv->K, 16) || !cc_aligned(kv->V, 16), CC_ERR_SHAPE, "K and V must be 16-byte aligned");
     return {CC_OK, ""};
 }
