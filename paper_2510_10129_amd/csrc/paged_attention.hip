@@ -526,6 +526,7 @@ template <int D_H, bool WIDE_PAGES>
 __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int per_min) {
     __shared__ __align__(16) bf16_t smem[LDS_TILES * BN_KEYS * D_H];
     __shared__ int simd_waves[4], group_waves[2], wave_units[8], last_here;
+    __shared__ struct { int longest, count; float sum; } of_wave[8];
     __shared__ int pre[MAX_BLOCKS + 1];
     __shared__ int e0[CC_PAGED_MAX_N + 1], rows_of[CC_PAGED_MAX_N], len_of[CC_PAGED_MAX_N];
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
@@ -541,6 +542,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         return b;
     };
     // ---- units in front of every block of a head ----
+    int aligned;
     {
         const int base = max(0, min(a.start[0], a.rows));
         for (int b = tid; b <= a.n; b += 512) {
@@ -554,18 +556,47 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         }
         __syncthreads();
         const int blocks = min(e0[a.n], MAX_BLOCKS);
+        int longest = 0, count = 0;
+        float sum = 0.0f;
+        for (int e = tid; e < blocks; e += 512) {
+            const int b = sequence_of(e), c0 = (e - e0[b]) * 256, n = rows_of[b], first = len_of[b] - n;
+            int len = 0;
+            if (c0 >= 0 && c0 < n * a.g) {
+                const int end = first + min(n - 1, (c0 + 255) / a.g) + 1;
+                len = visible_tiles(first + c0 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS).count + CHUNK_START;
+                longest = max(longest, len);
+                sum += len;
+                ++count;
+            }
+            pre[e] = len;
+        }
+        for (int off = 32; off > 0; off >>= 1) {
+            longest = max(longest, __shfl_xor(longest, off));
+            count += __shfl_xor(count, off);
+            sum += __shfl_xor(sum, off);
+        }
+        if (lane == 0) of_wave[w] = {longest, count, sum};
+        __syncthreads();
+        longest = count = 0;
+        sum = 0.0f;
+        for (int j = 0; j < 8; ++j) {
+            longest = max(longest, of_wave[j].longest);
+            count += of_wave[j].count;
+            sum += of_wave[j].sum;
+        }
+        // Ranges start with a block where equal ones would be hardly shorter: one with the end of a block and the start of
+        // another leaves two pieces.
+        const int in_all = count * a.H_kv, n_wg = gridDim.x;
+        aligned = 0;
+        if (count > 0 && in_all <= n_wg) {
+            const int cuts = n_wg / in_all, each = max(per_min, (longest + cuts - 1) / cuts);
+            if ((float)each <= 1.1f * sum * a.H_kv / n_wg + 2.0f) aligned = each;
+        }
         int carry = 0;
         for (int i0 = 0; i0 < blocks; i0 += 512) {
             const int e = i0 + tid;
-            int len = 0;
-            if (e < blocks) {
-                const int b = sequence_of(e);
-                const int c0 = (e - e0[b]) * 256, n = rows_of[b], first = len_of[b] - n;
-                if (c0 >= 0 && c0 < n * a.g) {
-                    const int end = first + min(n - 1, (c0 + 255) / a.g) + 1;
-                    len = visible_tiles(first + c0 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS).count + CHUNK_START;
-                }
-            }
+            int len = e < blocks ? pre[e] : 0;
+            if (aligned > 0) len = (len + aligned - 1) / aligned * aligned;
             int inc = len;
             for (int off = 1; off < 64; off <<= 1) {
                 const int v = __shfl_up(inc, off);
@@ -583,28 +614,31 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         }
         if (tid == 0) pre[blocks] = carry;
         __syncthreads();
+        aligned = uniform(aligned);
     }
     const int blocks = uniform(min(e0[a.n], MAX_BLOCKS)), head_units = uniform(pre[blocks]);
     const int64_t total = (int64_t)head_units * a.H_kv;
     const int n_wg = gridDim.x;
-    const int64_t per = max((int64_t)per_min, (total + n_wg - 1) / n_wg);
+    const int64_t per = aligned > 0 ? aligned : max((int64_t)per_min, (total + n_wg - 1) / n_wg);
     // workgroup ids go round-robin to the 8 XCDs: each gets consecutive ranges
     const int x = blockIdx.x & 7, xq = n_wg >> 3, xr = n_wg & 7;
     const int range = x * xq + min(x, xr) + (int)(blockIdx.x >> 3);
     int64_t u = range * per;
     const int64_t stop = min(u + per, total);
     while (u < stop) {
-        const int kvh = (int)(u / head_units), uh = (int)(u - (int64_t)kvh * head_units);
+        const int kvh = (int)quotient(u, head_units), uh = (int)(u - (int64_t)kvh * head_units);
         int e = 0;
         for (int i = lane; i - lane < blocks; i += 64) e += __popcll(__ballot(i < blocks && pre[min(i, blocks - 1) + 1] <= uh));
         e = uniform(e);
         const int b = uniform(sequence_of(e));
-        const int b0 = uniform(pre[e]), len = uniform(pre[e + 1]) - b0, rt = e - uniform(e0[b]);
+        const int b0 = uniform(pre[e]), padded = uniform(pre[e + 1]) - b0, rt = e - uniform(e0[b]);
         const batch_seq sq = seq_of(a, b);
         const int n_new = uniform(sq.n), L = uniform(sq.L), first = L - n_new;
-        const int ta = max(0, uh - b0 - CHUNK_START), te = (int)min((int64_t)len, uh - b0 + (stop - u)) - CHUNK_START;
+        const int end = first + min(n_new - 1, (rt * 256 + 255) / a.g) + 1;
+        const tile_span span = visible_tiles(first + rt * 256 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS);
+        const int ta = max(0, uh - b0 - CHUNK_START), te = min((int)min((int64_t)padded, uh - b0 + (stop - u)) - CHUNK_START, span.count);
         const int64_t u0 = (int64_t)kvh * head_units + b0;
-        u = u0 + len;
+        u = u0 + padded;
         if (te <= ta) continue;
         in_pages<WIDE_PAGES> keys;
         keys.table = (scalar_table)(a.p.table + uniform(sq.s) * a.p.st_table);
@@ -612,10 +646,9 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         keys.st_page = a.st_page, keys.st_tok = a.st_tok, keys.sh = a.st_head;
         keys.shift = a.p.shift, keys.n_pages = a.p.n_pages, keys.L = L, keys.first = first, keys.row0 = uniform(sq.row0);
         keys.window = a.window, keys.sinks = a.sinks;
-        const int end = first + min(n_new - 1, (rt * 256 + 255) / a.g) + 1;
-        keys.span = visible_tiles(first + rt * 256 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS);
-        const bool whole = ta == 0 && te == keys.span.count;
-        const int w0 = (int)((u0 + CHUNK_START) / per), w1 = (int)((u0 + len - 1) / per);
+        keys.span = span;
+        const bool whole = ta == 0 && te == span.count;
+        const int w0 = (int)quotient(u0 + CHUNK_START, per), w1 = (int)quotient(u0 + CHUNK_START + span.count - 1, per);
         attend<D_H, true, uint32_t>(keys, a.q, n_new, a.H_q, a.g, a.o, a.scale_log2, a.part, smem, grp, widx, kvh, rt, ta, te - ta,
                                     whole ? -1 : 2 * range + (w0 == range ? 1 : 0));
         if (whole) continue;
