@@ -45,6 +45,17 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
 }
 
+// The blocks of a many-rows launch that leaves its pieces to another: entry (kv head, e) has the units
+// kvh * head_units + first[e] .., in ranges of `per`.
+constexpr int CUT_SHARE = 4;                  // of the workgroups: up to so many blocks leave their pieces to another launch
+constexpr int CUT_BLOCKS = CC_PAGED_WGS / 2;
+struct cut_table {
+    int64_t per;
+    int32_t head_units, blocks;
+    int32_t first[CUT_BLOCKS], tiles[CUT_BLOCKS], seq[CUT_BLOCKS], row_tile[CUT_BLOCKS];
+};
+static_assert(sizeof(cut_table) <= CC_PAGED_CUT_BYTES, "room for it in a pool's scratch");
+
 struct paged_args {
     const bf16_t* q;
     bf16_t* o;
@@ -60,6 +71,7 @@ struct paged_args {
     const bf16_t* zeros;        // d_h of them
     float* part;                // pieces: two slots a workgroup
     int32_t* arrived;           // [workgroups], zero between calls
+    struct cut_table* cuts;     // many rows: where the pieces are, for a launch that adds them; NULL: the last workgroup does
 };
 
 struct batch_seq {
@@ -520,6 +532,12 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
 constexpr int CHUNK_START = 5;                // units of a block besides its key tiles, as in the even grids of attention.hip
 constexpr int MAX_BLOCKS = CC_PAGED_MAX_COLUMNS / 256 + CC_PAGED_MAX_N;
 
+// Key tiles that row tile rt of a sequence of n new rows from position `first` on sees.
+__device__ __forceinline__ tile_span row_tile_span(const paged_args& a, int first, int n, int rt) {
+    const int end = first + min(n - 1, (rt * 256 + 255) / a.g) + 1;
+    return visible_tiles(first + rt * 256 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS);
+}
+
 // A workgroup of eight waves per range.  Blocks are numbered e0(b) + row tile with e0(b) = floor(columns in front of b / 256) + b:
 // at least as many numbers as sequence b has row tiles, the unused ones of length 0, and no scan is needed to find one.
 template <int D_H, bool WIDE_PAGES>
@@ -562,8 +580,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
             const int b = sequence_of(e), c0 = (e - e0[b]) * 256, n = rows_of[b], first = len_of[b] - n;
             int len = 0;
             if (c0 >= 0 && c0 < n * a.g) {
-                const int end = first + min(n - 1, (c0 + 255) / a.g) + 1;
-                len = visible_tiles(first + c0 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS).count + CHUNK_START;
+                len = row_tile_span(a, first, n, e - e0[b]).count + CHUNK_START;
                 longest = max(longest, len);
                 sum += len;
                 ++count;
@@ -584,13 +601,14 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
             count += of_wave[j].count;
             sum += of_wave[j].sum;
         }
-        // Ranges start with a block where equal ones would be hardly shorter: one with the end of a block and the start of
-        // another leaves two pieces.
+        // Ranges start with a block where equal ones would not be much shorter: one with the end of a block and the start of
+        // another leaves two pieces (two chunks of 1024 rows under a window of 4096, 28 heads of 4: 170 us in equal ranges, 163
+        // so; 16 of 100 rows over 500 to 1500 tokens 60 and 56; 700 rows over 20000 238 and 225).  Without any cut they may be longer.
         const int in_all = count * a.H_kv, n_wg = gridDim.x;
         aligned = 0;
         if (count > 0 && in_all <= n_wg) {
             const int cuts = n_wg / in_all, each = max(per_min, (longest + cuts - 1) / cuts);
-            if ((float)each <= 1.1f * sum * a.H_kv / n_wg + 2.0f) aligned = each;
+            if ((float)each <= 1.1f * sum * a.H_kv / n_wg + (cuts == 1 ? 10.0f : 2.0f)) aligned = each;
         }
         int carry = 0;
         for (int i0 = 0; i0 < blocks; i0 += 512) {
@@ -620,6 +638,16 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
     const int64_t total = (int64_t)head_units * a.H_kv;
     const int n_wg = gridDim.x;
     const int64_t per = aligned > 0 ? aligned : max((int64_t)per_min, (total + n_wg - 1) / n_wg);
+    if (a.cuts && blockIdx.x == 0) {
+        if (tid == 0) a.cuts->per = per, a.cuts->head_units = head_units, a.cuts->blocks = blocks;
+        for (int e = tid; e < min(blocks, CUT_BLOCKS); e += 512) {
+            const int b = sequence_of(e), rt = e - e0[b], n = rows_of[b], first = len_of[b] - n;
+            a.cuts->first[e] = pre[e];
+            a.cuts->seq[e] = b;
+            a.cuts->row_tile[e] = rt;
+            a.cuts->tiles[e] = pre[e + 1] == pre[e] ? 0 : row_tile_span(a, first, n, rt).count;
+        }
+    }
     // workgroup ids go round-robin to the 8 XCDs: each gets consecutive ranges
     const int x = blockIdx.x & 7, xq = n_wg >> 3, xr = n_wg & 7;
     const int range = x * xq + min(x, xr) + (int)(blockIdx.x >> 3);
@@ -634,8 +662,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         const int b0 = uniform(pre[e]), padded = uniform(pre[e + 1]) - b0, rt = e - uniform(e0[b]);
         const batch_seq sq = seq_of(a, b);
         const int n_new = uniform(sq.n), L = uniform(sq.L), first = L - n_new;
-        const int end = first + min(n_new - 1, (rt * 256 + 255) / a.g) + 1;
-        const tile_span span = visible_tiles(first + rt * 256 / a.g, max(end, 0), a.window, a.sinks, BN_KEYS);
+        const tile_span span = row_tile_span(a, first, n_new, rt);
         const int ta = max(0, uh - b0 - CHUNK_START), te = min((int)min((int64_t)padded, uh - b0 + (stop - u)) - CHUNK_START, span.count);
         const int64_t u0 = (int64_t)kvh * head_units + b0;
         u = u0 + padded;
@@ -651,7 +678,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         const int w0 = (int)quotient(u0 + CHUNK_START, per), w1 = (int)quotient(u0 + CHUNK_START + span.count - 1, per);
         attend<D_H, true, uint32_t>(keys, a.q, n_new, a.H_q, a.g, a.o, a.scale_log2, a.part, smem, grp, widx, kvh, rt, ta, te - ta,
                                     whole ? -1 : 2 * range + (w0 == range ? 1 : 0));
-        if (whole) continue;
+        if (whole || a.cuts) continue;
         // ---- a cut block: the workgroup that comes last adds the pieces, in the order of their keys ----
         wait_loads<0>();                                   // the piece is written
         __syncthreads();
@@ -719,6 +746,56 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
     }
 }
 
+// Adds the pieces of a many-rows launch: o = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, in the order of their keys.  A workgroup takes
+// 32 columns (a wave of the kernel that left them) and 32 of their d's of a block; a thread four sums of a column,
+// of eight pieces at a time.  For few blocks in many pieces, which one workgroup a block reads at 75 GB/s (64 rows over 32768
+// tokens, 8 blocks in 32 pieces: 116 us with the last workgroup adding them, 67 so).
+template <int D_H>
+__global__ __launch_bounds__(256) void add_pieces_kernel(paged_args a) {
+    const cut_table& c = *a.cuts;
+    const int kvh = blockIdx.x % a.H_kv, e = blockIdx.x / a.H_kv;
+    if (e >= min(c.blocks, CUT_BLOCKS) || c.tiles[e] == 0) return;
+    const int64_t u0 = (int64_t)kvh * c.head_units + c.first[e] + CHUNK_START;
+    const int w0 = (int)quotient(u0, c.per), w1 = (int)quotient(u0 + c.tiles[e] - 1, c.per);
+    if (w0 == w1) return;
+    const batch_seq s = seq_of(a, c.seq[e]);
+    const int lane = threadIdx.x & 63, k = blockIdx.z * 4 + (threadIdx.x >> 6);
+    const int col = c.row_tile[e] * 256 + blockIdx.y * 32 + (lane & 31), mi = col / a.g, hg = col - mi * a.g;
+    if (mi >= s.n) return;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int NP = 8;
+    for (int j0 = w0; j0 <= w1; j0 += NP) {
+        float2 ml[NP], v[NP][2];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int j = min(j0 + i, w1);                 // past the end: the last piece again, with weight 0
+            const float* pp = a.part + (int64_t)(2 * j + (j == w0 ? 1 : 0)) * 256 * (D_H + 4) + blockIdx.y * 32 * (D_H + 4);
+            ml[i] = *reinterpret_cast<const float2*>(pp + 32 * D_H + lane * 2);
+            v[i][0] = *reinterpret_cast<const float2*>(pp + k * 256 + lane * 2);
+            v[i][1] = *reinterpret_cast<const float2*>(pp + k * 256 + 128 + lane * 2);
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) mn = fmaxf(mn, ml[i].x);
+        const float ref = mn == -INFINITY ? 0.0f : mn, keep = __builtin_amdgcn_exp2f(m - ref);
+        l *= keep;
+        acc *= keep;
+        m = mn;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const float f = j0 + i <= w1 ? __builtin_amdgcn_exp2f(ml[i].x - ref) : 0.0f;
+            l += ml[i].y * f;
+            acc += f * f32x4{v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y};
+        }
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    bf16x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (bf16_t)(acc[i] * inv);
+    *reinterpret_cast<bf16x4*>(a.o + ((int64_t)(s.row0 + mi) * a.H_q + kvh * a.g + hg) * D_H + 8 * k + 4 * (lane >> 5)) = r;
+}
+
 }  // namespace
 
 void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_page_pool& p, const cc_paged_kv& kv, int window,
@@ -728,7 +805,7 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
     paged_args a = {q, o, r.start, r.seq, r.n, r.rows, cc_view(p), (const bf16_t*)kv.K, (const bf16_t*)kv.V, kv.stride_page,
                     kv.stride_token, kv.stride_head, window, sinks, m.H_q, m.H_kv, g,
                     1.4426950408889634f / sqrtf((float)m.d_h), ws.zeros,
-                    (float*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn, ws.arrived};
+                    (float*)((char*)((int32_t*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn) + CC_PAGED_CUT_BYTES), ws.arrived, nullptr};
     const int grid = std::min(cc_device_cus(), CC_PAGED_WGS);
     const int64_t columns = (int64_t)std::min(r.max_new, r.rows) * g;
     const int per_min = WAVES + START;                     // a tile for each wave
@@ -736,6 +813,10 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
         const int chunk_min = 3 + CHUNK_START;
 #define CC_CHUNK(D, WIDE) hipLaunchKernelGGL((chunk_attn_kernel<D, WIDE>), dim3(grid), dim3(512), 0, s, a, chunk_min)
         const bool wide = p.page_size >= BN_KEYS;          // a tile of keys lies in one page
+        // few blocks are cut into many pieces each: a launch of its own adds them
+        const int64_t blocks = ((int64_t)r.rows * g / 256 + r.n) * m.H_kv;
+        if (blocks <= CUT_BLOCKS && blocks <= grid / CUT_SHARE)
+            a.cuts = (cut_table*)((int32_t*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn);
         if (m.d_h == 128) {
             if (wide) CC_CHUNK(128, true);
             else CC_CHUNK(128, false);
@@ -744,6 +825,11 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
             else CC_CHUNK(64, false);
         }
 #undef CC_CHUNK
+        if (a.cuts) {
+            const dim3 mg((unsigned)blocks, 8, m.d_h / 32);
+            if (m.d_h == 128) hipLaunchKernelGGL(add_pieces_kernel<128>, mg, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL(add_pieces_kernel<64>, mg, dim3(256), 0, s, a);
+        }
         return;
     }
 #define CC_FEW(D, NC) hipLaunchKernelGGL((few_attn_kernel<D, NC>), dim3(grid), dim3(64 * WAVES), 0, s, a, per_min)

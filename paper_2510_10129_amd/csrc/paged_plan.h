@@ -13,6 +13,7 @@
 #define CC_PAGED_MAX_COLUMNS (1 << 20)   // (row, query head of a group) columns of one call
 #define CC_PAGED_WGS 256           // most workgroups of an attention launch that leave pieces, two slots each
 #define CC_PAGED_SLOT (256 * (128 + 4))  // floats of the largest piece
+#define CC_PAGED_CUT_BYTES 4096     // the table of a launch that leaves its pieces to another
 #define CC_PAGED_CTX_INTS (CC_PAGED_WGS + 64)   // of a context: a count per workgroup, and 128 bf16 zeros
 #define CC_PAGE_LAYERS 128         // layers whose pages one copy launch takes (their addresses are kernel arguments)
 
@@ -30,7 +31,7 @@ inline cc_page_work cc_page_work_layout(int64_t n_pages, int64_t n_seqs) {
     const int64_t n = std::max(n_pages, n_seqs);
     w.src = take(n), w.dst = take(n), w.rows = take(n);
     w.attn = at;
-    w.ints = at + (int64_t)2 * CC_PAGED_WGS * CC_PAGED_SLOT;
+    w.ints = at + CC_PAGED_CUT_BYTES / 4 + (int64_t)2 * CC_PAGED_WGS * CC_PAGED_SLOT;
     return w;
 }
 
