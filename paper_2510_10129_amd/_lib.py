@@ -197,6 +197,14 @@ def _bf16(t, what: str):
     return t
 
 
+def _on(pool, *tensors):
+    """A host address, or one of another device, would fault the GPU."""
+    device = pool.refs.get_device()
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError("tensors must lie on the pool's device")
+
+
 class _Module:
     """torch, imported when first asked for something."""
 
@@ -251,9 +259,7 @@ class PagePool(_Described):
             self.work = torch.empty(size, dtype=torch.uint8, device=self.refs.device)
         if not self.work.is_contiguous():
             raise ValueError("work must be contiguous")
-        for t in (self.table, self.len, self.status, self.work):
-            if t.device != self.refs.device:
-                raise ValueError("a pool's tensors must lie on one device")
+        _on(self, self.table, self.len, self.status, self.work)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_seqs: int, max_pages: int, device="cuda"):
@@ -505,22 +511,24 @@ class Context:
         self._check(call(self._h, C.byref(p), *args, C.byref(host) if sync else None))
 
     @staticmethod
-    def _seqs(a, b):
+    def _seqs(pool: PagePool, a, b):
         if _i32(a, "sequences").numel() != _i32(b, "their second list").numel():
             raise ValueError("the two lists must have the same length")
+        _on(pool, a, b)
         return a.data_ptr(), b.data_ptr(), a.numel()
 
     def grow_pages(self, pool: PagePool, kvs: Sequence[PagedKV], seq, n_new, sync: bool = True):
         """Room for n_new[i] more tokens of sequence seq[i].  sync: waits for the device's status and raises on an error;
         without it pool.status says how the call ended (so for the three calls below)."""
         arr, n_layers = self._layers(pool, kvs)
-        self._pages(self._lib.cc_grow_pages, pool, sync, arr, n_layers, *self._seqs(seq, n_new))
+        self._pages(self._lib.cc_grow_pages, pool, sync, arr, n_layers, *self._seqs(pool, seq, n_new))
 
     def fork_pages(self, pool: PagePool, src, dst, sync: bool = True):
-        self._pages(self._lib.cc_fork_pages, pool, sync, *self._seqs(src, dst))
+        self._pages(self._lib.cc_fork_pages, pool, sync, *self._seqs(pool, src, dst))
 
     def free_pages(self, pool: PagePool, seq, sync: bool = True):
-        self._pages(self._lib.cc_free_pages, pool, sync, _i32(seq, "seq").data_ptr(), seq.numel())
+        _on(pool, _i32(seq, "seq"))
+        self._pages(self._lib.cc_free_pages, pool, sync, seq.data_ptr(), seq.numel())
 
     def compact_pages(self, pool: PagePool, kvs: Sequence[PagedKV], sync: bool = True):
         self._pages(self._lib.cc_compact_pages, pool, sync, *self._layers(pool, kvs))
@@ -540,6 +548,7 @@ class Context:
             raise ValueError("q_out must be contiguous")
         if pos is not None and _i32(pos, "pos").numel() < new.rows:
             raise ValueError("pos must have an entry for each row")
+        _on(pool, q, k, v, q_out, new.start, *(t for t in (new.seq, pos) if t is not None))
         p, kvs, r, rule = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct(), rope.c_struct()
         self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st[0], k.data_ptr(), st[1], v.data_ptr(), st[2], C.byref(r),
                                                   _ptr(pos), C.byref(p), C.byref(kvs), C.byref(rule), q_out.data_ptr(), flags))
@@ -550,6 +559,7 @@ class Context:
         for t, what in ((q, "q"), (o, "o")):
             if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
                 raise ValueError(f"{what} must be contiguous")
+        _on(pool, q, o, new.start, *(() if new.seq is None else (new.seq,)))
         p, kvs, r = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct()
         self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,
                                                       o.data_ptr(), flags))

@@ -278,6 +278,30 @@ def test_peaked_and_growing_scores():
         ctx.close()
 
 
+@pytest.mark.parametrize("seed", range(30))
+def test_batches_at_random(seed):
+    """Head layouts, page sizes, batches of 1 to 150 sequences, lengths of 1 to 9000, one to 600 rows, windows: whole blocks, blocks in
+    two and in dozens of pieces, ranges with the ends of two blocks; a few rows of each sequence are compared."""
+    rng = np.random.default_rng(1000 + seed)
+    d_h = int(rng.choice([64, 128]))
+    h_kv = int(rng.choice([1, 2, 4, 8]))
+    g = int(rng.choice([1, 3, 4, 7, 8]))
+    n = int(rng.choice([1, 1, 2, 5, 70, 150]))
+    most = int(min(9000, 40000 // n))
+    lens = [int(v) for v in np.exp(rng.uniform(0, np.log(most), size=n)).astype(int) + 1]
+    cap = int(rng.choice([1, 1, 4, 40, 600]))
+    news = [int(min(L, rng.integers(0 if n > 1 else 1, cap + 1))) for L in lens]
+    window = int(rng.choice([0, 0, rng.integers(1, 3000)]))
+    sinks = int(rng.integers(0, 130)) if window else 0
+    b = Batch(rng, h_kv * g, h_kv, d_h, int(rng.choice([16, 32, 64, 256])), lens, news, head_major=bool(rng.integers(2)), pad=(0, 1))
+    b.hide(0x7FC0)
+    ctx = _ctx(h_kv * g, h_kv, d_h)
+    o = b.device().attend(ctx, window, sinks)
+    b.check(o, window, sinks, sample=3)
+    assert torch.equal(b.attend(ctx, window, sinks).view(torch.int16), o.view(torch.int16))
+    ctx.close()
+
+
 # ---- rotary positions and the append ----
 
 def _rope_case(rng, b, rule, packed, pos=None, in_place=False):
@@ -483,6 +507,16 @@ def test_refusals_leave_no_trace():
     with pytest.raises(cc.CacheClipError) as e:
         ctx.free_pages(small, dev_i32([0]))
     assert e.value.status == _lib.CC_ERR_WORKSPACE
+    host, x = torch.zeros(1, dtype=torch.int32), torch.zeros((1, 256), dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: ctx.free_pages(pool, host), lambda: ctx.fork_pages(pool, dev_i32([0]), host),
+                 lambda: cc.PagePool(pool.refs, pool.table, pool.len.cpu(), 16),
+                 lambda: ctx.compact_pages(pool, [cc.PagedKV(K.cpu(), K.cpu())]),
+                 lambda: ctx.step_paged_attention(x, cc.NewRows(torch.tensor([0, 1], dtype=torch.int32), None, 1, 1), pool, kv, x.clone()),
+                 lambda: ctx.step_paged_attention(x.cpu(), cc.NewRows(dev_i32([0, 1]), None, 1, 1), pool, kv, x),
+                 lambda: ctx.step_rope_append(x, x[:, :128], x[:, :128], cc.NewRows(dev_i32([0, 1]), None, 1, 1), pool, kv, cc.Rope(1e4, 64), x,
+                                              pos=host)):
+        with pytest.raises(ValueError):                      # host memory does not reach the device
+            call()
     assert not pool.refs.any() and not pool.len.any()
     ctx.grow_pages(pool, [], dev_i32([]), dev_i32([]))       # nothing to do
     ctx.fork_pages(pool, dev_i32([]), dev_i32([]))

@@ -209,9 +209,9 @@ def test_binding_checks_buffers_before_the_call():
         ctx.step_rope_append(q, k, k, new, P, kv, rule, q, pos=torch.zeros(4, dtype=torch.int32))
     one = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError):
-        ctx._seqs(one, torch.zeros(2, dtype=torch.int32))
+        ctx._seqs(P, one, torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
-        ctx._seqs(one.long(), one)
+        ctx._seqs(P, one.long(), one)
 
 
 def test_null_context_is_refused():
