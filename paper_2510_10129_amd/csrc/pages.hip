@@ -349,7 +349,9 @@ enum { ROPE_HALVES = 0, ROPE_NEIGHBOURS = 1, ROPE_ODD_HALVES = 2 };
 // through), so that a pair meets in one lane and queries may be turned in place; where they are neighbours, 16 bytes.  Halves that
 // are no multiple of 16 bytes take the pairs' other members one by one; a head is then read by one wave before it is written.
 // Up to four passes over heads are loaded before the first is stored, the first of them before the row's place is looked up: a
-// chain of start, length and page.  A chunk's rows are bound by HBM, a few rows by that chain.
+// chain of start, length and page.  A chunk's rows are bound by HBM, a few rows by that chain.  Loads are non-temporal (what is
+// written is read next, what is read is not): rows from HBM, 4096 of 64 heads of 8 44 -> 37 us (4.5 TB/s read and written), 1024 of 32 of 8 12.4 -> 10.3,
+// 32 6.8 -> 6.6.
 template <int D_H, int MODE>
 __global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf16_t* q, int64_t st_q, const bf16_t* __restrict__ k,
                                                           int64_t st_k, const bf16_t* __restrict__ v, int64_t st_v,
@@ -380,8 +382,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf1
             const int h = hb + i * per_pass;
             if (my_head >= per_pass || h >= h_end) continue;
             const bf16_t* src = source(h) + e0;
-            x[i] = *reinterpret_cast<const bf16x8*>(src);
-            if (MODE == ROPE_HALVES && paired) y[i] = *reinterpret_cast<const bf16x8*>(src + half);
+            x[i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(src));
+            if (MODE == ROPE_HALVES && paired) y[i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(src + half));
             if (MODE == ROPE_ODD_HALVES && h < H_q + H_kv) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
