@@ -275,7 +275,8 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
  *   status  [1]                   result of the last of the four calls below: 0 or a cc_status
  *   work    cc_page_work_bytes(n_pages, n_seqs) bytes, 256-byte aligned: scratch, its contents mean nothing
  *           between calls.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
- *           at once), whatever context they come from.
+ *           at once), whatever context they come from; nor must two attention calls of one context, whatever
+ *           their pools.
  * page_size is a power of two, 16 to 1024; n_seqs <= 65536, n_pages * page_size < 2^31, max_pages * page_size < 2^30. */
 typedef struct cc_page_pool {
     int32_t* refs;
@@ -294,9 +295,10 @@ int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs);
 
 /* One layer's pages, dev bf16: element (page, token, head, c) of K and V is at
  * page*stride_page + token*stride_token + head*stride_head + c (elements; strides multiples of 8, c contiguous,
- * tokens or heads outermost in a page, stride_token < 2^23, page_size * stride_token < 2^31).  Slots behind a sequence's last token may hold anything; the others must be
- * finite, as everywhere in this library.  A page outside [0, n_pages) reads as zeros and is never written, so that
- * pages which slid out of every window may be given back. */
+ * tokens or heads outermost in a page, stride_token < 2^23, page_size * stride_token < 2^31).  Slots behind a
+ * sequence's last token may hold anything; the others must be finite, as everywhere in this library.  An entry outside
+ * [0, n_pages) reads as zeros and is never written: a program may take a page that slid out of every window back by itself,
+ * lowering its count by one and setting the entry to -1. */
 typedef struct cc_paged_kv {
     void* K;
     void* V;
@@ -323,7 +325,7 @@ typedef struct cc_new_rows {
  * during the call only, all with the same strides), so that it can be written to.  All or nothing: with too few free
  * pages status is CC_ERR_WORKSPACE, with more than max_pages for a sequence CC_ERR_SHAPE, with a bad or
  * repeated index CC_ERR_IDX, and nothing has changed.
- * status_host (host, or NULL): if given the call waits for the status and also returns it. */
+ * status_host (host, or NULL): if given the call waits for the status and also returns it (not while a graph is captured). */
 cc_status cc_grow_pages(cc_ctx* ctx, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers,
                         const int32_t* seq, const int32_t* n_new, int32_t n, int32_t* status_host);
 /* Sequence dst[i] (dev int32 [n], distinct, each of length 0) becomes a second holder of all that src[i] holds at the
@@ -333,7 +335,8 @@ cc_status cc_fork_pages(cc_ctx* ctx, const cc_page_pool* pool, const int32_t* sr
 /* Sequences seq[i] (dev int32 [n], distinct) give back what they hold; their lengths become 0. */
 cc_status cc_free_pages(cc_ctx* ctx, const cc_page_pool* pool, const int32_t* seq, int32_t n, int32_t* status_host);
 /* Moves the pages in use to the front: with L pages in use, the i-th of them that lies at L or behind goes to
- * the i-th free page in front of L, in every layer; refs and every sequence's entries follow. */
+ * the i-th free page in front of L, in every layer (kv: all that the pool's tables stand for); refs and every sequence's
+ * entries follow.  A page that a program holds by a count of its own, without an entry, moves too. */
 cc_status cc_compact_pages(cc_ctx* ctx, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers,
                            int32_t* status_host);
 
@@ -358,7 +361,8 @@ typedef struct cc_rope {
 
 /* Rotary positions of new rows and their keys and values into the pages.  q dev bf16 [rows, H_q*d_h], k and v
  * [rows, H_kv*d_h], row strides in elements (the three parts of one QKV product, for instance); q_out dev bf16
- * [rows, H_q*d_h], contiguous: the turned queries (it may be q itself where q's rows are contiguous).
+ * [rows, H_q*d_h], contiguous: the turned queries (it may be q itself where q's rows are contiguous; else it must not overlap
+ * q, k or v).
  * pos dev int32 [rows], or NULL: the position each row turns by where it is not the row's place in the sequence.
  * A sequence must not be listed twice, and a page that another sequence also holds is written all the same:
  * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths and the written pages first;
@@ -369,7 +373,7 @@ cc_status cc_step_rope_append(cc_ctx* ctx, const void* q, int64_t stride_q, cons
                               int32_t flags);
 /* Attention of new rows over the paged cache, grouped-query and causal: the row at position p sees key j <= p if window
  * is 0, j > p - window (the newest `window` keys, its own among them) or j < sinks.  q (turned) and o dev bf16
- * [rows, H_q*d_h].  A row that sees nothing (in front of its sequence's first token) gets zeros.
+ * [rows, H_q*d_h], not overlapping.  A row that sees nothing (in front of its sequence's first token) gets zeros.
  * flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths and the pages that some row sees first. */
 cc_status cc_step_paged_attention(cc_ctx* ctx, const void* q, const cc_new_rows* rows, const cc_page_pool* pool,
                                   const cc_paged_kv* kv, int32_t window, int32_t sinks, void* o, int32_t flags);

@@ -696,6 +696,10 @@ cc_status cc_step_rope_append(cc_ctx* c, const void* q, int64_t stride_q, const 
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out))
         return fail(c, CC_ERR_SHAPE, "buffers must be 16-byte aligned");
     if (q_out == q && stride_q != nq) return fail(c, CC_ERR_SHAPE, "q_out may be q only where q's rows are contiguous");
+    const int64_t last = rows->rows - 1, n_out = rows->rows * nq;
+    if ((q_out != q && cc_overlap(q_out, n_out, q, last * stride_q + nq)) || cc_overlap(q_out, n_out, k, last * stride_k + nk) ||
+        cc_overlap(q_out, n_out, v, last * stride_v + nk))
+        return fail(c, CC_ERR_SHAPE, "q_out must not overlap q, unless it is q, nor k or v");
     device_scope dev(c->device);
     if (flags & CC_FLAG_CHECK_IDX) {
         cc_status st = check_rows_sync(c, *rows, *pool, 0, 0, 1);
@@ -719,6 +723,8 @@ cc_status cc_step_paged_attention(cc_ctx* c, const void* q, const cc_new_rows* r
     if (rows->rows > 0 && (!q || !o)) return fail(c, CC_ERR_NULL, "q and o must not be NULL");
     CC_REFUSE(c, cc_check_attend(*rows, *pool, c->m.H_q / c->m.H_kv, window, sinks));
     if (!aligned16(q) || !aligned16(o)) return fail(c, CC_ERR_SHAPE, "buffers must be 16-byte aligned");
+    const int64_t n_q = (int64_t)rows->rows * c->m.H_q * c->m.d_h;
+    if (cc_overlap(q, n_q, o, n_q)) return fail(c, CC_ERR_SHAPE, "o must not overlap q");
     device_scope dev(c->device);
     if (flags & CC_FLAG_CHECK_IDX) {
         cc_status st = check_rows_sync(c, *rows, *pool, window, sinks, 0);

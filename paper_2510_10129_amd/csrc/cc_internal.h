@@ -46,7 +46,7 @@ struct cc_ctx {
     int32_t* n_sel;    // [1]
     int32_t* flag;     // [1] idx check result
     int32_t* paged;    // [CC_PAGED_CTX_INTS] counts of a paged attention's cut blocks (zero between calls), then d_h zeros
-    int32_t* pinned;   // host pinned [2]
+    int32_t* pinned;   // host pinned [4]
     int32_t* pinned_dev;   // the device's address of it
     cc_launch_override ovr;   // test overrides of the launch shapes (all zero: none)
 

@@ -36,12 +36,13 @@ void cc_launch_free(const cc_page_pool& p, const int32_t* seq, int n, int32_t* h
 void cc_launch_compact(const cc_page_pool& p, int32_t* host, hipStream_t s);
 // The copies that a grow or compact left in the pool's scratch, at most `most` of them, in every layer.
 void cc_launch_page_copies(const cc_page_pool& p, const cc_paged_kv* kv, int n_layers, int most, int H_kv, int d_h, hipStream_t s);
-// Sets *flag where a batch does not fit its pool.  low: pages that rows see (window, sinks); append: pages they are written to.
+// Sets *flag where a batch does not fit its pool.  Of its pages it looks at those that rows see (window, sinks), or with append at
+// those that they are written to.
 void cc_launch_check_rows(const cc_new_rows& r, const cc_page_pool& p, int window, int sinks, int append, int32_t* flag, hipStream_t s);
 void cc_launch_rope_append(const bf16_t* q, int64_t st_q, const bf16_t* k, int64_t st_k, const bf16_t* v, int64_t st_v,
                            const cc_new_rows& r, const int32_t* pos, const cc_page_pool& p, const cc_paged_kv& kv,
                            const cc_rope& rope, const cc_model_desc& m, bf16_t* q_out, hipStream_t s);
-// Of the context: d_h zeros, and a count per workgroup that is zero between calls.
+// Of the context: d_h zeros for keys that no page holds, and a count per workgroup that is zero between calls.
 struct cc_paged_scratch {
     const bf16_t* zeros;
     int32_t* arrived;

@@ -2,7 +2,7 @@
 //
 // Few rows (few_attn_kernel).  A sequence's new rows are a handful of (row, query head) columns per kv head, every key and
 // value is read once, and what bounds the call is how fast HBM delivers them: 512 bytes a key and head at d_h = 128
-// against 4 d_h flops a column, 16 to 64 columns.  So the chip is filled along the keys: the key tiles of all
+// against 4 d_h flops a column, 16 or 32 columns.  So the chip is filled along the keys: the key tiles of all
 // (sequence, kv head) blocks form one sequence of units that is cut into equal ranges, a workgroup each (one per CU), and a
 // block that a cut goes through is put together from its pieces by the workgroup that finishes it last.  Within a workgroup the
 // tiles of a block are dealt to four waves that run on their own: a wave keeps a ring of tiles of its own in LDS, filled by
@@ -749,7 +749,8 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
 // Adds the pieces of a many-rows launch: o = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, in the order of their keys.  A workgroup takes
 // 32 columns (a wave of the kernel that left them) and 32 of their d's of a block; a thread four sums of a column,
 // of eight pieces at a time.  For few blocks in many pieces, which one workgroup a block reads at 75 GB/s (64 rows over 32768
-// tokens, 8 blocks in 32 pieces: 116 us with the last workgroup adding them, 67 so).
+// tokens, 8 blocks in 32 pieces: 116 us with the last workgroup adding them, 60 so).  From a quarter as many blocks as workgroups on each
+// has four pieces at most, and the second launch costs more than it saves.
 template <int D_H>
 __global__ __launch_bounds__(256) void add_pieces_kernel(paged_args a) {
     const cut_table& c = *a.cuts;

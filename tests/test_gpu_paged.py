@@ -503,6 +503,15 @@ def test_refusals_leave_no_trace():
         with pytest.raises(cc.CacheClipError) as e:
             call()
         assert e.value.status == _lib.CC_ERR_SHAPE
+    buf, new = torch.zeros(4096, dtype=torch.bfloat16, device=DEV), cc.NewRows(dev_i32([0, 2]), None, 2, 2)
+    q, qkv = buf[:512].view(2, 256), buf.view(2, 2048)[:, :512]
+    for call in (lambda: ctx.step_paged_attention(q, new, pool, kv, q), lambda: ctx.step_paged_attention(q, new, pool, kv, buf[504:1016].view(2, 256)),
+                 lambda: ctx.step_rope_append(qkv[:, :256], qkv[:, 256:384], qkv[:, 384:], new, pool, kv, cc.Rope(1e4, 64), buf[248:760].view(2, 256)),
+                 lambda: ctx.step_rope_append(q, qkv[:, 256:384], buf[512:].view(2, 1792)[:, :128], new, pool, kv, cc.Rope(1e4, 64), q),
+                 lambda: ctx.step_rope_append(q, buf[1024:].view(2, 1536)[:, :128], qkv[:, 384:], new, pool, kv, cc.Rope(1e4, 64), q)):
+        with pytest.raises(cc.CacheClipError) as e:          # results over what is still read
+            call()
+        assert e.value.status == _lib.CC_ERR_SHAPE and "overlap" in str(e.value)
     small = cc.PagePool(pool.refs, pool.table, pool.len, 16, work=torch.zeros(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(cc.CacheClipError) as e:
         ctx.free_pages(small, dev_i32([0]))
@@ -643,7 +652,7 @@ def test_every_kernel_is_timed():
     ctx.profile_enable(True)
     ctx.grow_pages(pool, [kv], dev_i32([0]), dev_i32([1]))
     new = cc.NewRows(dev_i32([0, 1]), None, 1, 1)
-    ctx.step_rope_append(x, x[:, :128], x[:, :128], new, pool, kv, cc.Rope(1e4, 64), x)
+    ctx.step_rope_append(x, x[:, :128], x[:, :128], new, pool, kv, cc.Rope(1e4, 64), torch.empty_like(x))
     ctx.step_paged_attention(x, new, pool, kv, torch.empty_like(x))
     prof = ctx.profile_read()
     assert {k for k, (_, n) in prof.items() if n} == {"pages", "page_copy", "rope_append", "paged_attn"}

@@ -25,11 +25,12 @@ int list(int n, int n_seqs, const int32_t* a, const int32_t* b) { return cc_chec
 int new_rows(const cc_new_rows* r, int n_seqs, int g) { return cc_check_new_rows(r, n_seqs, g).code; }
 int rope(const cc_rope* r, int d_h) { return cc_check_rope(r, d_h).code; }
 void turns(const cc_rope* r, double* out) { cc_rope_turns(*r, out); }
+int overlap(const void* a, int64_t na, const void* b, int64_t nb) { return cc_overlap(a, na, b, nb); }
 int64_t work(int n_pages, int n_seqs) { return cc_page_work_size(n_pages, n_seqs); }
 void layout(int n_pages, int n_seqs, int64_t* o) {
     const cc_page_work w = cc_page_work_layout(n_pages, n_seqs);
-    const int64_t v[] = {w.mark, w.take, w.first, w.copy_at, w.list, w.list2, w.map, w.src, w.dst, w.rows, w.attn, w.ints};
-    for (int i = 0; i < 12; ++i) o[i] = v[i];
+    const int64_t v[] = {w.mark, w.take, w.first, w.copy_at, w.list, w.map, w.src, w.dst, w.rows, w.attn, w.ints};
+    for (int i = 0; i < 11; ++i) o[i] = v[i];
 }
 }
 """
@@ -77,13 +78,13 @@ def test_pool_checks(lib):
 
 @pytest.mark.parametrize("n_pages,n_seqs", [(1, 1), (64, 4), (7, 300), (100000, 65536)])
 def test_scratch_regions_do_not_overlap(lib, n_pages, n_seqs):
-    o = (C.c_int64 * 12)()
+    o = (C.c_int64 * 11)()
     lib.layout(n_pages, n_seqs, o)
-    sizes = [n_seqs] * 4 + [n_pages] * 3 + [max(n_pages, n_seqs)] * 3
+    sizes = [n_seqs] * 4 + [n_pages] * 2 + [max(n_pages, n_seqs)] * 3
     assert o[0] >= 2
     for i, n in enumerate(sizes):
         assert o[i] + n <= o[i + 1], i
-    assert o[10] <= o[11] and lib.work(n_pages, n_seqs) == 4 * o[11]
+    assert o[9] <= o[10] and lib.work(n_pages, n_seqs) == 4 * o[10]
 
 
 def test_layer_checks(lib):
@@ -142,6 +143,16 @@ def test_rope_frequencies(lib, kind, base, rot, orig, low, high):
     lib.turns(C.byref(rule.c_struct()), out)
     ref = paged.frequencies(base, rot, kind, 8.0, orig, low, high) / (2 * math.pi)
     assert np.allclose(out[:rot // 2], ref, rtol=1e-12)
+
+
+def test_overlap(lib):
+    def over(a, n_a, b, n_b):
+        assert lib.overlap(C.c_void_p(a), C.c_int64(n_a), C.c_void_p(b), C.c_int64(n_b)) == lib.overlap(
+            C.c_void_p(b), C.c_int64(n_b), C.c_void_p(a), C.c_int64(n_a))
+        return lib.overlap(C.c_void_p(a), C.c_int64(n_a), C.c_void_p(b), C.c_int64(n_b))
+
+    assert over(A, 8, A, 8) and over(A, 9, A + 16, 8) and over(A, 100, A + 32, 1) and over(A, 1 << 32, A + (1 << 33) - 2, 1)
+    assert not over(A, 8, A + 16, 8) and not over(A, 0, A, 8) and not over(A, 1 << 32, A + (1 << 33), 1)
 
 
 def _torch_pool(n_pages=8, page=16, n_seqs=3, max_pages=4):
