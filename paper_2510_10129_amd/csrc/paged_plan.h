@@ -17,16 +17,16 @@
 #define CC_PAGED_CTX_INTS (CC_PAGED_WGS + 64)   // of a context: a count per workgroup, and 128 bf16 zeros
 #define CC_PAGE_LAYERS 128         // layers whose pages one copy launch takes (their addresses are kernel arguments)
 
-// Scratch of a pool, in ints: a header, per sequence (marks, takes, offsets), per page (a list, a map), and the copies
+// Scratch of a pool, in ints: a header, per sequence (takes, offsets), per page (a list, a map), and the copies
 // that a call leaves for the copy kernel; behind it what an attention launch leaves (the table of its cuts, the pieces).
 struct cc_page_work {
-    int64_t mark, take, first, copy_at, list, map, src, dst, rows, attn, ints;
+    int64_t take, first, copy_at, list, map, src, dst, rows, attn, ints;
 };
 inline cc_page_work cc_page_work_layout(int64_t n_pages, int64_t n_seqs) {
     cc_page_work w;
     int64_t at = 64;                              // [0]: copies to make
     auto take = [&](int64_t n) { const int64_t a = at; at += (n + 63) / 64 * 64; return a; };
-    w.mark = take(n_seqs), w.take = take(n_seqs), w.first = take(n_seqs), w.copy_at = take(n_seqs);
+    w.take = take(n_seqs), w.first = take(n_seqs), w.copy_at = take(n_seqs);
     w.list = take(n_pages), w.map = take(n_pages);
     const int64_t n = std::max(n_pages, n_seqs);
     w.src = take(n), w.dst = take(n), w.rows = take(n);

@@ -10,6 +10,7 @@
 namespace {
 
 constexpr int NT = 1024;
+typedef int quad __attribute__((ext_vector_type(4), aligned(4)));   // of a list that is aligned to its entries only
 constexpr int ROWS = 8;                      // entries of a table row that a lane loads before it stores the first
 
 // Inclusive scan over the workgroup; every thread comes here.  part: NT / 64 entries of LDS.
@@ -40,104 +41,168 @@ __device__ __forceinline__ void finish(int32_t* status, int32_t* host, int bad) 
     if (host) *host = st;
 }
 
-// Sets BAD_INDEX where an index is out of range or repeated.  All threads; ends with a barrier.
-__device__ __forceinline__ void check_distinct(const int32_t* seq, int n, int n_seqs, int32_t* mark, int* bad) {
-    for (int i = threadIdx.x; i < n; i += NT) {
-        const int s = seq[i];
-        if ((unsigned)s < (unsigned)n_seqs) mark[s] = 0;
-        else atomicOr(bad, BAD_INDEX);
+// Sequences that a list has named: a bit each.
+struct seen_bits {
+    uint32_t word[65536 / 32];
+    __device__ __forceinline__ void clear() {
+        for (int i = threadIdx.x; i < 65536 / 32; i += NT) word[i] = 0;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += NT) {
-        const int s = seq[i];
-        if ((unsigned)s < (unsigned)n_seqs && atomicAdd(&mark[s], 1)) atomicOr(bad, BAD_INDEX);
+    // whether s is a sequence and named for the first time
+    __device__ __forceinline__ bool first(int s, int n_seqs) {
+        return (unsigned)s < (unsigned)n_seqs && !(atomicOr(&word[s >> 5], 1u << (s & 31)) >> (s & 31) & 1);
     }
-    __syncthreads();
-}
+};
 
+// A decode loop's every step comes here, and what it costs is its chain of round trips to memory.  So a thread keeps its entry
+// of the list in registers from its checks to its writes, the counts of the first pages are asked for before they are needed, and the pages
+// found wait in LDS; only lists of more than NT entries go through the pool's scratch.  36 entries with a copy each: 8.2 us (9.6 with
+// everything in scratch and a wave per entry); 1000 entries of three pages, a launch's 6 us among them, 25 (64).
 __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t* __restrict__ seq,
                                                   const int32_t* __restrict__ n_new, int n, int32_t* work, cc_page_work w,
                                                   int32_t* status, int32_t* host) {
-    __shared__ int bad;
+    constexpr int PER = 32;                           // pages a thread looks at in a step
+    constexpr int LIST = 4096;                        // pages found that LDS holds
+    constexpr int FEW = 5;                            // pages that a thread hands to its entry by itself
+    __shared__ seen_bits seen;
+    __shared__ int bad, big, list[LIST];
     __shared__ int64_t part[NT / 64];
-    const int tid = threadIdx.x, page = 1 << p.shift;
-    if (tid == 0) bad = 0, work[0] = 0;
-    __syncthreads();
-    check_distinct(seq, n, p.n_seqs, work + w.mark, &bad);
-    if (!(bad & BAD_INDEX))
-        for (int i = tid; i < n; i += NT) {
-            const int s = seq[i], c = n_new[i], L = p.len[s];
-            const int64_t to = (int64_t)L + c;
-            if (c < 0 || L < 0) { atomicOr(&bad, BAD_INDEX); continue; }
-            if (to > (int64_t)p.max_pages << p.shift) { atomicOr(&bad, BAD_LENGTH); continue; }
-            const int have = (L + page - 1) >> p.shift;
-            int copy = 0;
-            if (c > 0 && (L & (page - 1))) {
-                const int last = p.table[s * p.st_table + have - 1];
-                if ((unsigned)last >= (unsigned)p.n_pages) { atomicOr(&bad, BAD_INDEX); continue; }
-                copy = p.refs[last] > 1;
-            }
-            work[w.take + i] = 2 * ((int)((to + page - 1) >> p.shift) - have + copy) + copy;
+    __shared__ int part32[NT / 64];
+    __shared__ struct { int64_t row; int at, all; } hand[NT];
+    const int tid = threadIdx.x, lane = tid & 63, page = 1 << p.shift;
+    // the free ones among the thread's pages from p0 on
+    auto look = [&](int64_t p0) -> unsigned {
+        const int64_t a = p0 + (int64_t)tid * PER;
+        unsigned free = 0;
+        if (a + PER <= p.n_pages) {
+            quad x[PER / 4];
+#pragma unroll
+            for (int k = 0; k < PER / 4; ++k) x[k] = *reinterpret_cast<const quad*>(p.refs + a + 4 * k);
+#pragma unroll
+            for (int k = 0; k < PER; ++k) free |= (unsigned)(x[k / 4][k % 4] == 0) << k;
+        } else if (a < p.n_pages) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) free |= (unsigned)(p.refs[min(a + k, (int64_t)p.n_pages - 1)] == 0 && a + k < p.n_pages) << k;
         }
+        return free;
+    };
+    const int s0 = tid < n ? seq[tid] : 0, c0 = tid < n ? n_new[tid] : 0;
+    const unsigned free0 = look(0);
+    seen.clear();
+    if (tid == 0) bad = big = 0, work[0] = 0;
+    __syncthreads();
+
+    // t: twice the pages that an entry takes, plus one if one of them is for a copy; before: pages and copies (the upper part) of
+    // the entries in front of it
+    struct entry { int s, c, L, t, old; int64_t before; };
+    auto entry_of = [&](int i) -> entry {
+        entry e = {};
+        if (i < n) e.s = seq[i], e.c = n_new[i], e.L = p.len[e.s], e.t = work[w.take + i];
+        return e;
+    };
+    constexpr int64_t COPY = (int64_t)1 << 40;
+    entry mine = {};
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + tid;
+        entry e = {};
+        int wrong = 0;
+        if (i < n) {
+            e.s = i0 == 0 ? s0 : seq[i], e.c = i0 == 0 ? c0 : n_new[i];
+            if (!seen.first(e.s, p.n_seqs)) {
+                wrong = BAD_INDEX;
+            } else {
+                e.L = p.len[e.s];
+                const int64_t to = (int64_t)e.L + e.c;
+                if (e.c < 0 || e.L < 0) wrong = BAD_INDEX;
+                else if (to > (int64_t)p.max_pages << p.shift) wrong = BAD_LENGTH;
+                else {
+                    const int have = (e.L + page - 1) >> p.shift;
+                    int copy = 0;
+                    if (e.c > 0 && (e.L & (page - 1))) {
+                        e.old = p.table[e.s * p.st_table + have - 1];
+                        if ((unsigned)e.old >= (unsigned)p.n_pages) wrong = BAD_INDEX;
+                        else copy = p.refs[e.old] > 1;
+                    }
+                    e.t = 2 * ((int)((to + page - 1) >> p.shift) - have + copy) + copy;
+                }
+            }
+        }
+        if (wrong) atomicOr(&bad, wrong);
+        if (i0 == 0) mine = e;
+        else if (i < n) work[w.take + i] = e.t;
+    }
     __syncthreads();
     if (bad) return finish(status, host, bad);
 
-    // pages taken and copies made before entry i (copies in the upper half of a 64-bit sum)
     int64_t carry = 0;
     for (int i0 = 0; i0 < n; i0 += NT) {
-        const int i = i0 + tid;
-        const int t = i < n ? work[w.take + i] : 0;
-        const int64_t mine = (t >> 1) + ((int64_t)(t & 1) << 40);
+        const int i = i0 + tid, t = i0 == 0 ? mine.t : i < n ? work[w.take + i] : 0;
+        const int64_t own = (t >> 1) + (t & 1) * COPY;
         int64_t sum;
-        const int64_t before = carry + block_scan(mine, part, sum) - mine;
-        if (i < n) {
-            work[w.first + i] = (int)min(before & ((1ll << 40) - 1), (int64_t)1 << 30);
+        const int64_t before = carry + block_scan(own, part, sum) - own;
+        if (i0 == 0) {
+            mine.before = before;
+        } else if (i < n) {
+            work[w.first + i] = (int)min(before & (COPY - 1), (int64_t)1 << 30);
             work[w.copy_at + i] = (int)(before >> 40);
         }
         carry += sum;
     }
-    const int64_t total = carry & ((1ll << 40) - 1);
+    const int64_t total = carry & (COPY - 1);
     const int copies = (int)(carry >> 40);
 
-    // the lowest free pages, eight consecutive pages a thread and step, until there are enough
-    constexpr int PER = 8;
-    int64_t found = 0;
+    // the lowest free pages until there are enough (a step is a round trip and a scan whatever it looks at: behind 150000 pages
+    // in use 97 us with 8 a thread, 33 with 32)
+    int found = 0;
     for (int64_t p0 = 0; p0 < p.n_pages && found < total; p0 += NT * PER) {
-        const int64_t a = p0 + (int64_t)tid * PER;
-        unsigned free = 0;
-#pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if (a + k < p.n_pages && p.refs[a + k] == 0) free |= 1u << k;
-        int64_t sum;
-        int64_t at = found + block_scan((int64_t)__popc(free), part, sum) - __popc(free);
-        for (; free; free &= free - 1, ++at)
-            if (at < total) work[w.list + at] = (int)(a + __ffs(free) - 1);
+        unsigned free = p0 == 0 ? free0 : look(p0);
+        int sum, at = found + block_scan((int)__popc(free), part32, sum) - (int)__popc(free);
+#pragma unroll 1
+        for (; free; free &= free - 1, ++at) {
+            const int q = (int)(p0 + (int64_t)tid * PER + __ffs(free) - 1);
+            if (at < LIST) list[at] = q;
+            else if (at < total) work[w.list + at] = q;
+        }
         found += sum;
     }
     __syncthreads();
     if (found < total) return finish(status, host, NO_PAGES);
+    auto page_at = [&](int k) -> int { return k < LIST ? list[k] : work[w.list + k]; };
 
-    const int lane = tid & 63;
-    for (int i = tid >> 6; i < n; i += NT / 64) {             // a wave per entry
-        const int s = seq[i], c = n_new[i], L = p.len[s], copy = work[w.take + i] & 1;
-        const int have = (L + page - 1) >> p.shift, fresh = (work[w.take + i] >> 1) - copy;
-        int32_t* row = p.table + s * p.st_table;
-        const int32_t* mine = work + w.list + work[w.first + i];
-        if (copy && lane == 0) {
-            const int k = work[w.copy_at + i], old = row[have - 1];
-            work[w.src + k] = old;
-            work[w.dst + k] = mine[0];
-            work[w.rows + k] = L & (page - 1);
-            atomicSub(&p.refs[old], 1);
-            p.refs[mine[0]] = 1;
-            row[have - 1] = mine[0];
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + tid;
+        entry e = mine;
+        if (i0 > 0) {
+            e = entry_of(i);
+            if (i < n) e.before = work[w.first + i] + work[w.copy_at + i] * COPY;
         }
-        for (int k = lane; k < fresh; k += 64) {
-            const int q = mine[copy + k];
-            row[have + k] = q;
+        const int copy = e.t & 1, all = e.t >> 1, have = (e.L + page - 1) >> p.shift, at = (int)(e.before & (COPY - 1));
+        int32_t* row = p.table + e.s * p.st_table + have - copy;
+        if (copy) {
+            const int k = (int)(e.before >> 40), old = i0 == 0 ? e.old : row[0];
+            work[w.src + k] = old;
+            work[w.dst + k] = page_at(at);
+            work[w.rows + k] = e.L & (page - 1);
+            atomicSub(&p.refs[old], 1);
+        }
+#pragma unroll 1
+        for (int k = 0; k < min(all, FEW); ++k) {
+            const int q = page_at(at + k);
+            row[k] = q;
             p.refs[q] = 1;
         }
-        if (lane == 0) p.len[s] = L + c;
+        if (i < n) p.len[e.s] = e.L + e.c;
+        // more than a few: by whole waves
+        hand[tid] = {e.s * p.st_table + have - copy, at, all};
+        if (all > FEW) big = 1;
+        __syncthreads();
+        if (big)
+            for (int j = tid >> 6; j < min(NT, n - i0); j += NT / 64)
+                for (int k = FEW + lane; k < hand[j].all; k += 64) {
+                    const int q = page_at(hand[j].at + k);
+                    p.table[hand[j].row + k] = q;
+                    p.refs[q] = 1;
+                }
+        __syncthreads();
     }
     if (tid == 0) work[0] = copies;
     finish(status, host, 0);
@@ -148,29 +213,26 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
 __global__ __launch_bounds__(NT) void fork_kernel(cc_pool_view p, const int32_t* __restrict__ src,
                                                   const int32_t* __restrict__ dst, int n, int32_t* work, cc_page_work w,
                                                   int32_t* status, int32_t* host) {
+    __shared__ seen_bits seen;
     __shared__ int bad;
     const int tid = threadIdx.x, page = 1 << p.shift;
-    int32_t *taken = work + w.mark, *copies = work + w.first, *len = work + w.take, *leads = work + w.copy_at;
+    int32_t *copies = work + w.first, *len = work + w.take, *leads = work + w.copy_at;
+    seen.clear();
     if (tid == 0) bad = 0;
     __syncthreads();
     for (int i = tid; i < n; i += NT) {
         const int s = src[i], d = dst[i];
-        if ((unsigned)s >= (unsigned)p.n_seqs || (unsigned)d >= (unsigned)p.n_seqs || p.len[d] != 0) {
+        if ((unsigned)s >= (unsigned)p.n_seqs || !seen.first(d, p.n_seqs) || p.len[d] != 0) {
             atomicOr(&bad, BAD_INDEX);
         } else {
-            taken[d] = 0;
             copies[s] = 0;
             len[i] = cc_seq_len(p, s);                        // as it is at the call
         }
     }
     __syncthreads();
     if (bad) return finish(status, host, bad);
-    for (int i = tid; i < n; i += NT) {
-        if (atomicAdd(&taken[dst[i]], 1)) atomicOr(&bad, BAD_INDEX);
-        leads[i] = atomicAdd(&copies[src[i]], 1) == 0;
-    }
+    for (int i = tid; i < n; i += NT) leads[i] = atomicAdd(&copies[src[i]], 1) == 0;
     __syncthreads();
-    if (bad) return finish(status, host, bad);
     const int lane = tid & 63;
     for (int i = tid >> 6; i < n; i += NT / 64) {
         const int s = src[i], d = dst[i], L = len[i], held = (L + page - 1) >> p.shift, more = leads[i] ? copies[s] : 0;
@@ -192,13 +254,17 @@ __global__ __launch_bounds__(NT) void fork_kernel(cc_pool_view p, const int32_t*
     finish(status, host, 0);
 }
 
-__global__ __launch_bounds__(NT) void free_kernel(cc_pool_view p, const int32_t* __restrict__ seq, int n, int32_t* work,
-                                                  cc_page_work w, int32_t* status, int32_t* host) {
+__global__ __launch_bounds__(NT) void free_kernel(cc_pool_view p, const int32_t* __restrict__ seq, int n, int32_t* status,
+                                                  int32_t* host) {
+    __shared__ seen_bits seen;
     __shared__ int bad;
     const int tid = threadIdx.x, page = 1 << p.shift;
+    seen.clear();
     if (tid == 0) bad = 0;
     __syncthreads();
-    check_distinct(seq, n, p.n_seqs, work + w.mark, &bad);
+    for (int i = tid; i < n; i += NT)
+        if (!seen.first(seq[i], p.n_seqs)) atomicOr(&bad, BAD_INDEX);
+    __syncthreads();
     if (bad) return finish(status, host, bad);
     const int lane = tid & 63;
     for (int i = tid >> 6; i < n; i += NT / 64) {
@@ -471,8 +537,7 @@ void cc_launch_fork(const cc_page_pool& p, const int32_t* src, const int32_t* ds
                        cc_page_work_layout(p.n_pages, p.n_seqs), p.status, host);
 }
 void cc_launch_free(const cc_page_pool& p, const int32_t* seq, int n, int32_t* host, hipStream_t s) {
-    hipLaunchKernelGGL(free_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), seq, n, (int32_t*)p.work,
-                       cc_page_work_layout(p.n_pages, p.n_seqs), p.status, host);
+    hipLaunchKernelGGL(free_kernel, dim3(1), dim3(NT), 0, s, cc_view(p), seq, n, p.status, host);
 }
 void cc_launch_compact(const cc_page_pool& p, int32_t* host, hipStream_t s) {
     const cc_page_work w = cc_page_work_layout(p.n_pages, p.n_seqs);

@@ -29,8 +29,8 @@ int overlap(const void* a, int64_t na, const void* b, int64_t nb) { return cc_ov
 int64_t work(int n_pages, int n_seqs) { return cc_page_work_size(n_pages, n_seqs); }
 void layout(int n_pages, int n_seqs, int64_t* o) {
     const cc_page_work w = cc_page_work_layout(n_pages, n_seqs);
-    const int64_t v[] = {w.mark, w.take, w.first, w.copy_at, w.list, w.map, w.src, w.dst, w.rows, w.attn, w.ints};
-    for (int i = 0; i < 11; ++i) o[i] = v[i];
+    const int64_t v[] = {w.take, w.first, w.copy_at, w.list, w.map, w.src, w.dst, w.rows, w.attn, w.ints};
+    for (int i = 0; i < 10; ++i) o[i] = v[i];
 }
 }
 """
@@ -78,13 +78,13 @@ def test_pool_checks(lib):
 
 @pytest.mark.parametrize("n_pages,n_seqs", [(1, 1), (64, 4), (7, 300), (100000, 65536)])
 def test_scratch_regions_do_not_overlap(lib, n_pages, n_seqs):
-    o = (C.c_int64 * 11)()
+    o = (C.c_int64 * 10)()
     lib.layout(n_pages, n_seqs, o)
-    sizes = [n_seqs] * 4 + [n_pages] * 2 + [max(n_pages, n_seqs)] * 3
+    sizes = [n_seqs] * 3 + [n_pages] * 2 + [max(n_pages, n_seqs)] * 3
     assert o[0] >= 2
     for i, n in enumerate(sizes):
         assert o[i] + n <= o[i + 1], i
-    assert o[9] <= o[10] and lib.work(n_pages, n_seqs) == 4 * o[10]
+    assert o[8] <= o[9] and lib.work(n_pages, n_seqs) == 4 * o[9]
 
 
 def test_layer_checks(lib):
