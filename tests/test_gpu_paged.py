@@ -468,6 +468,38 @@ def test_random_histories(seed, n_pages, page, n_seqs, max_pages, layers, d_h, h
     ctx.close()
 
 
+def test_lists_longer_than_a_workgroup():
+    """More entries than threads, more pages than are found in one step, entries of none to many pages, copies in every part."""
+    rng = np.random.default_rng(31)
+    n_seqs, n_pages, page, max_pages = 5000, 40001, 16, 64
+    ctx = _ctx(1, 1, 64)
+    pool, P = cc.PagePool.empty(n_pages, page, n_seqs, max_pages, device=DEV), paged.Pages(n_pages, page, n_seqs, max_pages)
+    mirror = [[_bf16(rng, (n_pages, page, 1, 64)) for _ in range(2)]]
+    kvs = [cc.PagedKV(dev_bf16(K), dev_bf16(V)) for K, V in mirror]
+    order = rng.permutation(n_seqs).tolist()
+    first, rest = order[:2300], order[2300:]
+    more = [int(x) for x in rng.choice([0, 1, 15, 16, 17, 33, 81, 97, 640], size=2300, p=[.1, .2, .1, .1, .1, .2, .1, .05, .05])]
+    src = rng.choice(first, size=2500).tolist()
+    fine = rng.permutation(first + rest[:2500]).tolist()
+    steps = [("grow", first, more), ("fork", src, rest[:2500]), ("grow", fine, rng.integers(0, 40, size=4800).tolist()),
+             ("grow", fine + [fine[4000]], [1] * 4801), ("free", fine[::3], None), ("grow", fine[1::3], [300] * 1600),
+             ("grow", fine[1:3900:3], [300] * 1300)]
+    for kind, a, b in steps:
+        P.copies, got = [], 0
+        call = dict(grow=lambda: ctx.grow_pages(pool, kvs, dev_i32(a), dev_i32(b)), fork=lambda: ctx.fork_pages(pool, dev_i32(a), dev_i32(b)),
+                    free=lambda: ctx.free_pages(pool, dev_i32(a)))[kind]
+        want = P.free(a) if kind == "free" else getattr(P, kind)(a, b)
+        try:
+            call()
+        except cc.CacheClipError as e:
+            got = e.status
+        assert got == STATUS[want], (kind, want, got)
+        if want is None:
+            _apply(P, mirror)
+        _compare(pool, P, kvs, mirror)
+    ctx.close()
+
+
 def test_many_layers_take_several_launches():
     """More layers than one copy launch takes; a cow copy of 1 and of 15 tokens and a compaction."""
     rng = np.random.default_rng(30)
