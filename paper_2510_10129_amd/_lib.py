@@ -283,18 +283,23 @@ class PagedKV(_Described):
         K, V = _bf16(self.K, "K"), _bf16(self.V, "V")
         if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.stride(3) != 1 or K.device != V.device:
             raise ValueError("K and V must be of one shape, [n_pages, page_size, H_kv, d_h], with equal strides, the last of them 1")
-        return (K.data_ptr(), V.data_ptr()) + K.stride()[:3], tuple(K.shape), K.get_device()
+        fields = (K.data_ptr(), V.data_ptr()) + K.stride()[:3]
+        return fields, tuple(K.shape), K.get_device(), _PagedKV(*fields)
 
     @staticmethod
     def table(kvs: Sequence["PagedKV"], pool: PagePool, model):
         """The fields of a cc_paged_kv for each of kvs, one after the other, if the pages are those of the pool and the model."""
         want, device, flat = (pool.c_struct().n_pages, pool.page_size, model.H_kv, model.d_h), pool.refs.get_device(), []
         for kv in kvs:
-            fields, shape, lies_on = kv._c or kv.c_struct()
+            fields, shape, lies_on, _ = kv._c or kv.c_struct()
             if shape != want or lies_on != device:
                 raise ValueError(f"K and V are {shape} on device {lies_on}; the pool and the model want {want} on {device}")
             flat += fields
         return flat
+
+    def checked(self, pool: PagePool, model) -> _PagedKV:
+        self.table((self,), pool, model)
+        return self._c[3]
 
 
 @dataclass
@@ -541,16 +546,19 @@ class Context:
 
     def step_rope_append(self, q, k, v, new: NewRows, pool: PagePool, kv: PagedKV, rope: Rope, q_out, pos=None, flags: int = 0):
         """q [rows, H_q*d_h], k, v [rows, H_kv*d_h] cuda bf16 (column slices of one product will do) -> q_out, pages of kv."""
-        m = self.desc
-        nq, nk = m.H_q * m.d_h, m.H_kv * m.d_h
-        st = [self._row_buffer(t, w, new.rows, n) for t, w, n in ((q, "q", nq), (k, "k", nk), (v, "v", nk))]
-        if self._row_buffer(q_out, "q_out", new.rows, nq) != nq:
+        m, rows, row = self.desc, new.rows, self._row_buffer
+        d_h = m.d_h
+        nq, nk = m.H_q * d_h, m.H_kv * d_h
+        st_q, st_k, st_v = row(q, "q", rows, nq), row(k, "k", rows, nk), row(v, "v", rows, nk)
+        if row(q_out, "q_out", rows, nq) != nq:
             raise ValueError("q_out must be contiguous")
-        if pos is not None and _i32(pos, "pos").numel() < new.rows:
-            raise ValueError("pos must have an entry for each row")
-        _on(pool, q, k, v, q_out, new.start, *(t for t in (new.seq, pos) if t is not None))
-        p, kvs, r, rule = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct(), rope.c_struct()
-        self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st[0], k.data_ptr(), st[1], v.data_ptr(), st[2], C.byref(r),
+        if pos is not None:
+            if _i32(pos, "pos").numel() < rows:
+                raise ValueError("pos must have an entry for each row")
+            _on(pool, pos)
+        _on(pool, q, k, v, q_out, new.start) if new.seq is None else _on(pool, q, k, v, q_out, new.start, new.seq)
+        p, kvs, r, rule = pool.c_struct(), kv.checked(pool, m), new.c_struct(), rope.c_struct()
+        self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st_q, k.data_ptr(), st_k, v.data_ptr(), st_v, C.byref(r),
                                                   _ptr(pos), C.byref(p), C.byref(kvs), C.byref(rule), q_out.data_ptr(), flags))
 
     def step_paged_attention(self, q, new: NewRows, pool: PagePool, kv: PagedKV, o, window: int = 0, sinks: int = 0, flags: int = 0):
@@ -560,7 +568,7 @@ class Context:
             if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
                 raise ValueError(f"{what} must be contiguous")
         _on(pool, q, o, new.start, *(() if new.seq is None else (new.seq,)))
-        p, kvs, r = pool.c_struct(), _PagedKV(*PagedKV.table((kv,), pool, m)), new.c_struct()
+        p, kvs, r = pool.c_struct(), kv.checked(pool, m), new.c_struct()
         self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,
                                                       o.data_ptr(), flags))
 
