@@ -283,23 +283,22 @@ class PagedKV(_Described):
         K, V = _bf16(self.K, "K"), _bf16(self.V, "V")
         if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.stride(3) != 1 or K.device != V.device:
             raise ValueError("K and V must be of one shape, [n_pages, page_size, H_kv, d_h], with equal strides, the last of them 1")
-        fields = (K.data_ptr(), V.data_ptr()) + K.stride()[:3]
-        return fields, tuple(K.shape), K.get_device(), _PagedKV(*fields)
+        one = _PagedKV(K.data_ptr(), V.data_ptr(), *K.stride()[:3])
+        return bytes(one), (*K.shape, K.get_device()), one
 
     @staticmethod
-    def table(kvs: Sequence["PagedKV"], pool: PagePool, model):
-        """The fields of a cc_paged_kv for each of kvs, one after the other, if the pages are those of the pool and the model."""
-        want, device, flat = (pool.c_struct().n_pages, pool.page_size, model.H_kv, model.d_h), pool.refs.get_device(), []
-        for kv in kvs:
-            fields, shape, lies_on, _ = kv._c or kv.c_struct()
-            if shape != want or lies_on != device:
-                raise ValueError(f"K and V are {shape} on device {lies_on}; the pool and the model want {want} on {device}")
-            flat += fields
-        return flat
+    def table(kvs: Sequence["PagedKV"], pool: PagePool, model) -> array:
+        """A cc_paged_kv (two addresses, three strides) for each of kvs, if their pages are those of the pool and the model."""
+        want = (pool.c_struct().n_pages, pool.page_size, model.H_kv, model.d_h, pool.refs.get_device())
+        layers = [kv._c or kv.c_struct() for kv in kvs]
+        for layer in layers:
+            if layer[1] != want:
+                raise ValueError(f"K and V are {layer[1][:4]} on device {layer[1][4]}; the pool and the model want {want[:4]} on {want[4]}")
+        return array("q", b"".join([layer[0] for layer in layers]))
 
     def checked(self, pool: PagePool, model) -> _PagedKV:
         self.table((self,), pool, model)
-        return self._c[3]
+        return self._c[2]
 
 
 @dataclass
@@ -508,8 +507,8 @@ class Context:
 
     # ---- the paged cache of the answer phase ----
     def _layers(self, pool: PagePool, kvs: Sequence[PagedKV]):
-        n = len(kvs)                            # a _PagedKV is two addresses and three strides
-        return (_PagedKV * n).from_buffer(array("q", PagedKV.table(kvs, pool, self.desc))) if n else None, n
+        n = len(kvs)
+        return (_PagedKV * n).from_buffer(PagedKV.table(kvs, pool, self.desc)) if n else None, n
 
     def _pages(self, call, pool: PagePool, sync: bool, *args):
         p, host = pool.c_struct(), C.c_int32(0)

@@ -173,9 +173,9 @@ def test_binding_refuses_what_the_library_cannot_read():
         cc.PagePool(torch.zeros(16, **i32)[::2], P.table, P.len, 16)
     m = _lib.ModelDesc(64, 4, 2, 64, 64, 1e4, 1e-5, 64, 64, 64)
     K = torch.zeros(8, 16, 2, 64, dtype=torch.bfloat16)
-    assert cc.PagedKV.table([cc.PagedKV(K, K)], P, m)[2:] == [16 * 2 * 64, 2 * 64, 64]
+    assert cc.PagedKV.table([cc.PagedKV(K, K)], P, m).tolist()[2:] == [16 * 2 * 64, 2 * 64, 64]
     by_head = torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16).transpose(1, 2)
-    assert cc.PagedKV.table([cc.PagedKV(by_head, by_head)], P, m)[2:] == [16 * 2 * 64, 64, 16 * 64]
+    assert cc.PagedKV.table([cc.PagedKV(by_head, by_head)], P, m).tolist()[2:] == [16 * 2 * 64, 64, 16 * 64]
     for bad in (K.float(), K[:4], K[..., :32], K.transpose(2, 3).contiguous().transpose(2, 3), by_head):
         with pytest.raises(ValueError):
             cc.PagedKV.table([cc.PagedKV(K, bad)], P, m)
