@@ -15,12 +15,13 @@ constexpr int BN_KEYS = 64;
 // Rewriting M0 between loads is expensive while MFMAs are in flight (measured:
 // several hundred cycles per rewrite with two MFMA-bound waves on a SIMD), so
 // the loads of one tile and tensor share one base and differ in OFF only.
-template <int OFF>
+// STREAM: non-temporal.
+template <int OFF, bool STREAM = false>
 __device__ __forceinline__ void dma16(const bf16_t* gsrc_minus_off, bf16_t* lds_wave_base) {
     static_assert(OFF >= 0 && OFF < 4096, "the instruction offset is 13 bits signed; a larger value wraps silently");
     __builtin_amdgcn_global_load_lds(
         (const void __attribute__((address_space(1)))*)gsrc_minus_off,
-        (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, 0);
+        (void __attribute__((address_space(3)))*)lds_wave_base, 16, OFF, STREAM ? 2 : 0);
 }
 // LDS reads whose place in the instruction stream is fixed by the source order (the
 // compiler's scheduler, short of registers, would issue every read right before its use).
@@ -142,10 +143,11 @@ __device__ __forceinline__ tile_span visible_tiles(int first, int end, int windo
 // Keys and values in pages: row i of a sequence's new rows sits at position first + i.  The visible key tiles of a
 // row tile are `span`'s; within them a row sees key j up to its position, if it is within its window or a sink.
 // WIDE_PAGES: pages of 64 tokens and more, so that a tile lies in one; else every 16 keys have a page of their own.
+// ONCE: no other workgroup reads the same keys, so that they go past the caches.
 typedef const __attribute__((address_space(4))) int32_t* scalar_table;   // constant for the launch: scalar loads
-template <bool WIDE_PAGES>
+template <bool WIDE_PAGES, bool ONCE>
 struct in_pages {
-    static constexpr bool paged = true, wide_pages = WIDE_PAGES;
+    static constexpr bool paged = true, wide_pages = WIDE_PAGES, once = ONCE;
     scalar_table table;             // of the sequence
     const bf16_t* K;
     const bf16_t* V;
@@ -300,7 +302,7 @@ __device__ __forceinline__ void attend(
         if constexpr (Keys::paged) {
             Off off = tile.there[NB == 1 ? 0 : i] ? loff[i] : (Off)(l_col * 2);
             asm volatile("" : "+v"(off));
-            dma16<i * 1024>(reinterpret_cast<const bf16_t*>(b + off), stage + wave_slot);
+            dma16<i * 1024, Keys::once>(reinterpret_cast<const bf16_t*>(b + off), stage + wave_slot);
         } else {
             asm volatile("" : "+v"(loff[i]));   // keeps the (32-bit) offset a register operand of the load
             dma16<i * 1024>(reinterpret_cast<const bf16_t*>(b + loff[i]), stage + wave_slot);

@@ -540,7 +540,7 @@ __device__ __forceinline__ tile_span row_tile_span(const paged_args& a, int firs
 
 // A workgroup of eight waves per range.  Blocks are numbered e0(b) + row tile with e0(b) = floor(columns in front of b / 256) + b:
 // at least as many numbers as sequence b has row tiles, the unused ones of length 0, and no scan is needed to find one.
-template <int D_H, bool WIDE_PAGES>
+template <int D_H, bool WIDE_PAGES, bool ONCE>
 __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int per_min) {
     __shared__ __align__(16) bf16_t smem[LDS_TILES * BN_KEYS * D_H];
     __shared__ int simd_waves[4], group_waves[2], wave_units[8], last_here;
@@ -667,7 +667,7 @@ __global__ __launch_bounds__(512, 1) void chunk_attn_kernel(paged_args a, int pe
         const int64_t u0 = (int64_t)kvh * head_units + b0;
         u = u0 + padded;
         if (te <= ta) continue;
-        in_pages<WIDE_PAGES> keys;
+        in_pages<WIDE_PAGES, ONCE> keys;
         keys.table = (scalar_table)(a.p.table + uniform(sq.s) * a.p.st_table);
         keys.K = a.K, keys.V = a.V, keys.zeros = a.zeros;
         keys.st_page = a.st_page, keys.st_tok = a.st_tok, keys.sh = a.st_head;
@@ -812,18 +812,25 @@ void cc_launch_paged_attention(const bf16_t* q, const cc_new_rows& r, const cc_p
     const int per_min = WAVES + START;                     // a tile for each wave
     if (!cc_few_rows(columns, m.d_h)) {
         const int chunk_min = 3 + CHUNK_START;
-#define CC_CHUNK(D, WIDE) hipLaunchKernelGGL((chunk_attn_kernel<D, WIDE>), dim3(grid), dim3(512), 0, s, a, chunk_min)
+#define CC_CHUNK(D, WIDE, ONCE) hipLaunchKernelGGL((chunk_attn_kernel<D, WIDE, ONCE>), dim3(grid), dim3(512), 0, s, a, chunk_min)
+        // Keys that few rows read, and no other workgroup, go past the caches: 4 tokens over 4 times 65000, 64 heads of 8, 202 -> 173 us,
+        // 5 over 16 ragged sequences of up to 16581, 32 of 8, 141 -> 125, 8 over 4 of 8000 38.6 -> 38.3.  More columns leave less of
+        // the time to the loads and gain only where the last cache is too small, 64 over 16 of up to 16000 212 -> 207, 16 over
+        // 8 of 8000 58 -> 60.
+        const bool once = columns <= 32;
         const bool wide = p.page_size >= BN_KEYS;          // a tile of keys lies in one page
         // few blocks are cut into many pieces each: a launch of its own adds them
         const int64_t blocks = ((int64_t)r.rows * g / 256 + r.n) * m.H_kv;
         if (blocks <= CUT_BLOCKS && blocks <= grid / CUT_SHARE)
             a.cuts = (cut_table*)((int32_t*)p.work + cc_page_work_layout(p.n_pages, p.n_seqs).attn);
         if (m.d_h == 128) {
-            if (wide) CC_CHUNK(128, true);
-            else CC_CHUNK(128, false);
+            if (wide && once) CC_CHUNK(128, true, true);
+            else if (wide) CC_CHUNK(128, true, false);
+            else if (once) CC_CHUNK(128, false, true);
+            else CC_CHUNK(128, false, false);
         } else {
-            if (wide) CC_CHUNK(64, true);
-            else CC_CHUNK(64, false);
+            if (wide) CC_CHUNK(64, true, false);           // (so few are the other kernel's)
+            else CC_CHUNK(64, false, false);
         }
 #undef CC_CHUNK
         if (a.cuts) {
