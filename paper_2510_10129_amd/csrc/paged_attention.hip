@@ -12,10 +12,17 @@
 // A wave computes S^T = K Q^T and O^T = V^T P^T with 16x16x32 MFMAs, columns on the N side: a lane then owns one
 // column, its scores are laid out as the second product's operand needs them, and the rescale factor is one number per
 // lane.  The running maximum moves only when a score exceeds it by more than 2^8 (in base 2), so most tiles need neither an
-// exchange between lanes nor a rescale; probabilities up to 2^8 in bf16 and sums in fp32 cancel in the final division.
+// exchange between lanes nor a rescale; probabilities up to 2^8 and sums in fp32 cancel in the final division.  Probabilities
+// meet the values in two bf16 parts, what the first one's rounding left is the second, so that 2^-16 of them is lost: the matrix pipe
+// has the time (one token of 32 ragged sequences of up to 16577, 32 heads of 8, us with one part / two: d_h 128 236 / 234, d_h 64
+// 136 / 140).
 //
 // Many rows (chunk_attn_kernel): the loop of the contiguous cache's attention (attend.h), 256 columns a workgroup, with the
-// key tiles of all (sequence, row tile, kv head) blocks in equal ranges, and pieces put together as above.
+// key tiles of all (sequence, row tile, kv head) blocks in equal ranges, and pieces put together as above.  Probabilities are
+// rounded to bf16, 2^-8 of each at most, as there.  Two parts would take half as many matrix operations again and some
+// more vector ones, on pipes that bound these calls (us with one part / two: 1024 rows over 66560, 64 heads of 8, 2003 / 2697; 2 times
+// 1024 under a window of 4096, 28 of 4, 150 / 195; 6 times up to 512 over 4224, 32 of 8, d_h 64, 104 / 121; 5 drafted
+// tokens of 16 sequences of up to 16581, 32 of 8, where one wave of a workgroup has columns, 133 / 153).
 #include "attend.h"
 #include "paged.h"
 
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             }
             // a block of columns at a time: scores, mask, softmax in base 2 with the scale folded into the exponent
             const bool masked = key0 + KEYS - 1 > least || (a.window > 0 && key0 <= most - a.window && key0 + KEYS > a.sinks);
-            bf16x8 pf[NC];
+            bf16x8 pf[NC], pr[NC];                         // probabilities: bf16, and what that left of them
 #pragma unroll
             for (int nc = 0; nc < NC; ++nc) {
                 f32x4 sc[2];
@@ -383,6 +390,7 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
                         const float p = __builtin_amdgcn_exp2f(fmaf(sc[t][v], a.scale_log2, -ref));
                         l_run[nc] += p;
                         pf[nc][t * 4 + v] = (bf16_t)p;
+                        pr[nc][t * 4 + v] = (bf16_t)(p - (float)pf[nc][t * 4 + v]);
                     }
             }
             // ---- O^T += V^T P^T: the 32 keys in the order in which a lane holds its scores ----
@@ -405,12 +413,14 @@ __global__ __launch_bounds__(512, 2) void few_attn_kernel(paged_args a, int per_
             }
             ahead[0] = pages_of(k + 1 + NS);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const bf16x8 vf = __builtin_shufflevector(va[dt], vb[dt], 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int nc = 0; nc < NC; ++nc)
-                    acc[dt][nc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[nc], acc[dt][nc], 0, 0, 0);
-            }
+                for (int dt = 0; dt < DT; ++dt) {
+                    const bf16x8 vf = __builtin_shufflevector(va[dt], vb[dt], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                    for (int nc = 0; nc < NC; ++nc)
+                        acc[dt][nc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, part ? pr[nc] : pf[nc], acc[dt][nc], 0, 0, 0);
+                }
         }
 
         // ---- the four waves' sums together, as the registers lie: [dt][nc][lane]; to the output or to a piece (two lots of
