@@ -273,6 +273,10 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
  *           are not read (cc_free_pages leaves -1 there)
  *   len     [n_seqs]              tokens; 0 = the row is free
  *   status  [1]                   result of the last of the four calls below: 0 or a cc_status
+ *   refused [n_seqs], or NULL     0, or the cc_status with which the last cc_grow_pages that asked for tokens of this sequence was
+ *           refused.  The caller clears it at first; after that a grow of the sequence that is made, or freeing it, sets it to 0
+ *           (so may the caller).  While it is not 0, cc_step_rope_append skips the sequence's rows: their places do not exist, and
+ *           the last ones of the unchanged length hold other tokens.  NULL is for programs that wait for every grow's status.
  *   work    cc_page_work_bytes(n_pages, n_seqs) bytes, 256-byte aligned: scratch, its contents mean nothing
  *           between calls.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
  *           at once), whatever context they come from; nor must two attention calls of one context, whatever
@@ -290,6 +294,7 @@ typedef struct cc_page_pool {
     int32_t page_size;
     int32_t n_seqs;
     int32_t max_pages;
+    int32_t* refused;
 } cc_page_pool;
 int64_t cc_page_work_bytes(int32_t n_pages, int32_t n_seqs);
 
@@ -324,8 +329,9 @@ typedef struct cc_new_rows {
  * it first takes a page for a copy of that page's tokens, made in every layer (kv: host array [n_layers], read
  * during the call only, all with the same strides), so that it can be written to.  All or nothing: with too few free
  * pages status is CC_ERR_WORKSPACE, with more than max_pages for a sequence CC_ERR_SHAPE, with a bad or
- * repeated index CC_ERR_IDX, and nothing has changed.
- * status_host (host, or NULL): if given the call waits for the status and also returns it (not while a graph is captured). */
+ * repeated index CC_ERR_IDX, and nothing has changed but pool->refused of the listed sequences that asked for tokens.
+ * status_host (host, or NULL): if given the call waits for the status and also returns it (not while a graph is captured); if not,
+ * pool->refused must be there. */
 cc_status cc_grow_pages(cc_ctx* ctx, const cc_page_pool* pool, const cc_paged_kv* kv, int32_t n_layers,
                         const int32_t* seq, const int32_t* n_new, int32_t n, int32_t* status_host);
 /* Sequence dst[i] (dev int32 [n], distinct, each of length 0) becomes a second holder of all that src[i] holds at the
@@ -365,8 +371,9 @@ typedef struct cc_rope {
  * q, k or v).
  * pos dev int32 [rows], or NULL: the position each row turns by where it is not the row's place in the sequence.
  * A sequence must not be listed twice, and a page that another sequence also holds is written all the same:
- * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths and the written pages first;
- * without it, rows in front of their sequence's first token are skipped. */
+ * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths, the written pages and that no grow of
+ * a sequence with rows was refused first; without it, rows in front of their sequence's first token and rows of a sequence whose grow
+ * was refused are skipped: no key, value or query of theirs is written. */
 cc_status cc_step_rope_append(cc_ctx* ctx, const void* q, int64_t stride_q, const void* k, int64_t stride_k,
                               const void* v, int64_t stride_v, const cc_new_rows* rows, const int32_t* pos,
                               const cc_page_pool* pool, const cc_paged_kv* kv, const cc_rope* rope, void* q_out,

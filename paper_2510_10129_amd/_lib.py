@@ -72,7 +72,7 @@ class LaunchOverride(C.Structure):
 class _Pool(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("refs", "table", "len", "status", "work")] + [
         ("work_bytes", C.c_int64), ("stride_table", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32),
-        ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
+        ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("refused", C.c_void_p)]
 
 
 class _PagedKV(C.Structure):
@@ -236,14 +236,16 @@ class _Described:
 @dataclass
 class PagePool(_Described):
     """Pages that sequences hold by reference: refs [n_pages], table [n_seqs, max_pages], len [n_seqs] int32 on
-    the device, page_size tokens a page.  status and work are allocated where they are not given.  `PagePool.empty`
-    makes one with every page free."""
+    the device, page_size tokens a page.  status, work and refused (int32 [n_seqs]: 0, or why the last grow that asked for tokens of
+    the sequence was refused; `step_rope_append` skips its rows then) are allocated where they are not given.
+    `PagePool.empty` makes one with every page free."""
     refs: "object"
     table: "object"
     len: "object"
     page_size: int
     status: "object" = None
     work: "object" = None
+    refused: "object" = None
 
     def __post_init__(self):
         torch = _torch
@@ -259,7 +261,11 @@ class PagePool(_Described):
             self.work = torch.empty(size, dtype=torch.uint8, device=self.refs.device)
         if not self.work.is_contiguous():
             raise ValueError("work must be contiguous")
-        _on(self, self.table, self.len, self.status, self.work)
+        if self.refused is None:
+            self.refused = torch.zeros_like(self.len)
+        if _i32(self.refused, "refused").numel() != self.len.numel():
+            raise ValueError("refused must have an entry for each sequence")
+        _on(self, self.table, self.len, self.status, self.work, self.refused)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_seqs: int, max_pages: int, device="cuda"):
@@ -269,7 +275,7 @@ class PagePool(_Described):
     def _describe(self) -> _Pool:
         return _Pool(self.refs.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.status.data_ptr(),
                      self.work.data_ptr(), self.work.numel() * self.work.element_size(), self.table.stride(0),
-                     self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1])
+                     self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1], self.refused.data_ptr())
 
 
 @dataclass
@@ -523,7 +529,8 @@ class Context:
 
     def grow_pages(self, pool: PagePool, kvs: Sequence[PagedKV], seq, n_new, sync: bool = True):
         """Room for n_new[i] more tokens of sequence seq[i].  sync: waits for the device's status and raises on an error;
-        without it pool.status says how the call ended (so for the three calls below)."""
+        without it pool.status says how the call ended (so for the three calls below), until the next of them, and pool.refused
+        whose tokens have no room, until a grow of the sequence is made."""
         arr, n_layers = self._layers(pool, kvs)
         self._pages(self._lib.cc_grow_pages, pool, sync, arr, n_layers, *self._seqs(pool, seq, n_new))
 
@@ -544,7 +551,8 @@ class Context:
         return st[0] if rows > 1 else width
 
     def step_rope_append(self, q, k, v, new: NewRows, pool: PagePool, kv: PagedKV, rope: Rope, q_out, pos=None, flags: int = 0):
-        """q [rows, H_q*d_h], k, v [rows, H_kv*d_h] cuda bf16 (column slices of one product will do) -> q_out, pages of kv."""
+        """q [rows, H_q*d_h], k, v [rows, H_kv*d_h] cuda bf16 (column slices of one product will do) -> q_out, pages of kv.  Rows of
+        a sequence whose last grow was refused (pool.refused) are skipped."""
         m, rows, row = self.desc, new.rows, self._row_buffer
         d_h = m.d_h
         nq, nk = m.H_q * d_h, m.H_kv * d_h

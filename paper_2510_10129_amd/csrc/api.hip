@@ -125,7 +125,7 @@ cc_status check_rows_sync(cc_ctx* c, const cc_new_rows& r, const cc_page_pool& p
     CC_HIP(c, hipMemcpyAsync(c->pinned, c->flag, sizeof(int32_t), hipMemcpyDeviceToHost, c->stream));
     CC_HIP(c, hipStreamSynchronize(c->stream));
     if (c->pinned[0] != 0)
-        return fail(c, CC_ERR_IDX, "start must ascend within rows, seq be in range, a sequence be as long as its new rows and its pages be in range");
+        return fail(c, CC_ERR_IDX, "start must ascend within rows, seq be in range, a sequence be as long as its new rows, its pages be in range and its last grow not be refused");
     return CC_OK;
 }
 
@@ -628,6 +628,7 @@ cc_status cc_grow_pages(cc_ctx* c, const cc_page_pool* pool, const cc_paged_kv* 
     CC_REFUSE(c, cc_check_pool(pool));
     CC_REFUSE(c, cc_check_layers(kv, n_layers, pool->page_size, c->m.H_kv, c->m.d_h));
     CC_REFUSE(c, cc_check_list(n, pool->n_seqs, seq, n_new));
+    CC_REFUSE(c, cc_check_grow(*pool, status_host));
     device_scope dev(c->device);
     {
         cc_prof_scope ps(c, CC_K_PAGES);

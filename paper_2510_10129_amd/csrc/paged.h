@@ -8,18 +8,27 @@ struct cc_pool_view {
     int32_t* refs;
     int32_t* table;
     int32_t* len;
+    int32_t* refused;               // or NULL
     int64_t st_table;
     int32_t n_pages, n_seqs, max_pages;
     int32_t shift;                  // log2(page_size)
 };
 inline cc_pool_view cc_view(const cc_page_pool& p) {
-    return {p.refs, p.table, p.len, p.stride_table, p.n_pages, p.n_seqs, p.max_pages, __builtin_ctz(p.page_size)};
+    return {p.refs, p.table, p.len, p.refused, p.stride_table, p.n_pages, p.n_seqs, p.max_pages, __builtin_ctz(p.page_size)};
 }
 
 // Tokens of sequence s as far as its table can hold them; 0 for an index that is none.
 __device__ __forceinline__ int cc_seq_len(const cc_pool_view& p, int s) {
     if ((unsigned)s >= (unsigned)p.n_seqs) return 0;
     return max(0, min(p.len[s], p.max_pages << p.shift));
+}
+
+// The same for rows that are to be written: none where the sequence's last grow was refused, as its last places hold other
+// tokens then.
+__device__ __forceinline__ int cc_append_len(const cc_pool_view& p, int s) {
+    if ((unsigned)s >= (unsigned)p.n_seqs) return 0;
+    const int refused = p.refused ? p.refused[s] : 0, len = cc_seq_len(p, s);
+    return refused ? 0 : len;
 }
 
 // Sequence of the batch that row r belongs to (uniform in the wave; all lanes come here), -1: none.

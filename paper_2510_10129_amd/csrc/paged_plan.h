@@ -69,9 +69,15 @@ inline cc_refusal cc_check_pool(const cc_page_pool* p) {
                  CC_ERR_SHAPE, "n_pages * page_size must be below 2^31, max_pages * page_size below 2^30");
     CC_REFUSE_IF(p->stride_table < p->max_pages, CC_ERR_SHAPE, "stride_table must be at least max_pages");
     CC_REFUSE_IF(!cc_aligned(p->refs, 4) || !cc_aligned(p->table, 4) || !cc_aligned(p->len, 4) || !cc_aligned(p->status, 4) ||
-                     !cc_aligned(p->work, 256), CC_ERR_SHAPE, "tables must be 4-byte aligned and work 256-byte aligned");
+                     !cc_aligned(p->refused, 4) || !cc_aligned(p->work, 256), CC_ERR_SHAPE, "tables must be 4-byte aligned and work 256-byte aligned");
     CC_REFUSE_IF(p->work_bytes < cc_page_work_size(p->n_pages, p->n_seqs), CC_ERR_WORKSPACE,
                  "work holds less than cc_page_work_bytes(n_pages, n_seqs)");
+    return {CC_OK, ""};
+}
+
+// A grow that nobody waits for says what it refused to the append behind it.
+inline cc_refusal cc_check_grow(const cc_page_pool& p, const int32_t* status_host) {
+    CC_REFUSE_IF(!status_host && !p.refused, CC_ERR_NULL, "a grow without status_host needs pool->refused");
     return {CC_OK, ""};
 }
 

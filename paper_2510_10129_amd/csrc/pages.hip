@@ -34,9 +34,12 @@ __device__ __forceinline__ T block_scan(T v, T* part, T& total) {
 }
 
 enum { BAD_INDEX = 1, BAD_LENGTH = 2, NO_PAGES = 4 };
+__device__ __forceinline__ int status_of(int bad) {
+    return bad & BAD_INDEX ? CC_ERR_IDX : bad & BAD_LENGTH ? CC_ERR_SHAPE : bad & NO_PAGES ? CC_ERR_WORKSPACE : CC_OK;
+}
 __device__ __forceinline__ void finish(int32_t* status, int32_t* host, int bad) {
     if (threadIdx.x) return;
-    const int st = bad & BAD_INDEX ? CC_ERR_IDX : bad & BAD_LENGTH ? CC_ERR_SHAPE : bad & NO_PAGES ? CC_ERR_WORKSPACE : CC_OK;
+    const int st = status_of(bad);
     *status = st;
     if (host) *host = st;
 }
@@ -69,6 +72,13 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
     __shared__ int part32[NT / 64];
     __shared__ struct { int64_t row; int at, all; } hand[NT];
     const int tid = threadIdx.x, lane = tid & 63, page = 1 << p.shift;
+    // nothing changes but what the append looks at: who asked for tokens and got none
+    auto refuse = [&](int why) {
+        if (p.refused)
+            for (int i = tid; i < n; i += NT)
+                if ((unsigned)seq[i] < (unsigned)p.n_seqs && n_new[i] != 0) p.refused[seq[i]] = status_of(why);
+        finish(status, host, why);
+    };
     // the free ones among the thread's pages from p0 on
     auto look = [&](int64_t p0) -> unsigned {
         const int64_t a = p0 + (int64_t)tid * PER;
@@ -131,7 +141,7 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
         else if (i < n) work[w.take + i] = e.t;
     }
     __syncthreads();
-    if (bad) return finish(status, host, bad);
+    if (bad) return refuse(bad);
 
     int64_t carry = 0;
     for (int i0 = 0; i0 < n; i0 += NT) {
@@ -165,7 +175,7 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
         found += sum;
     }
     __syncthreads();
-    if (found < total) return finish(status, host, NO_PAGES);
+    if (found < total) return refuse(NO_PAGES);
     auto page_at = [&](int k) -> int { return k < LIST ? list[k] : work[w.list + k]; };
 
     for (int i0 = 0; i0 < n; i0 += NT) {
@@ -190,7 +200,10 @@ __global__ __launch_bounds__(NT) void grow_kernel(cc_pool_view p, const int32_t*
             row[k] = q;
             p.refs[q] = 1;
         }
-        if (i < n) p.len[e.s] = e.L + e.c;
+        if (i < n) {
+            p.len[e.s] = e.L + e.c;
+            if (p.refused && e.c > 0) p.refused[e.s] = 0;
+        }
         // more than a few: by whole waves
         hand[tid] = {e.s * p.st_table + have - copy, at, all};
         if (all > FEW) big = 1;
@@ -281,7 +294,10 @@ __global__ __launch_bounds__(NT) void free_kernel(cc_pool_view p, const int32_t*
                 if ((unsigned)q[k] < (unsigned)p.n_pages) atomicSub(&p.refs[q[k]], 1);
             }
         }
-        if (lane == 0) p.len[s] = 0;
+        if (lane == 0) {
+            p.len[s] = 0;
+            if (p.refused) p.refused[s] = 0;
+        }
     }
     finish(status, host, 0);
 }
@@ -390,7 +406,7 @@ __global__ __launch_bounds__(64) void check_rows_kernel(const int32_t* __restric
     bool bad = r0 < 0 || r1 < r0 || r1 > rows || (unsigned)s >= (unsigned)p.n_seqs;
     if (!bad) {
         const int n = r1 - r0, L = p.len[s];
-        bad = L < n || L > (int64_t)p.max_pages << p.shift;
+        bad = L < n || L > (int64_t)p.max_pages << p.shift || (append && n > 0 && p.refused && p.refused[s] != 0);
         if (!bad && n > 0) {
             const int first = L - n;
             const int low = append ? first : window > 0 ? max(0, first - window + 1) : 0;
@@ -465,7 +481,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(rope_args a, const bf1
     int at = -1, page = -1;
     if (b >= 0) {
         const int s = seq ? seq[b] : b;
-        const int L = cc_seq_len(p, s);
+        const int L = cc_append_len(p, s);
         at = L - start[b + 1] + r;
         if (at >= 0 && at < L) page = p.table[s * p.st_table + (at >> p.shift)];
         else at = -1;
