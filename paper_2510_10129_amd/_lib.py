@@ -249,20 +249,24 @@ class PagePool(_Described):
 
     def __post_init__(self):
         torch = _torch
-        _i32(self.refs, "refs"), _i32(self.table, "table", 2), _i32(self.len, "len")
-        if self.table.shape[0] != self.len.shape[0]:
-            raise ValueError("table and len must have a row for each sequence")
+        _i32(self.refs, "refs"), _i32(self.len, "len")
         if self.status is None:
             self.status = torch.zeros(1, dtype=torch.int32, device=self.refs.device)
-        if _i32(self.status, "status").numel() < 1:
-            raise ValueError("status must hold one value")
         if self.work is None:
             size = load_library().cc_page_work_bytes(self.refs.numel(), self.len.numel())
             self.work = torch.empty(size, dtype=torch.uint8, device=self.refs.device)
-        if not self.work.is_contiguous():
-            raise ValueError("work must be contiguous")
         if self.refused is None:
             self.refused = torch.zeros_like(self.len)
+        self._check()
+
+    def _check(self):
+        _i32(self.refs, "refs"), _i32(self.table, "table", 2), _i32(self.len, "len")
+        if self.table.shape[0] != self.len.shape[0]:
+            raise ValueError("table and len must have a row for each sequence")
+        if _i32(self.status, "status").numel() < 1:
+            raise ValueError("status must hold one value")
+        if not self.work.is_contiguous():
+            raise ValueError("work must be contiguous")
         if _i32(self.refused, "refused").numel() != self.len.numel():
             raise ValueError("refused must have an entry for each sequence")
         _on(self, self.table, self.len, self.status, self.work, self.refused)
@@ -273,6 +277,7 @@ class PagePool(_Described):
         return cls(_torch.zeros(n_pages, **i32), _torch.full((n_seqs, max_pages), -1, **i32), _torch.zeros(n_seqs, **i32), page_size)
 
     def _describe(self) -> _Pool:
+        self._check()
         return _Pool(self.refs.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.status.data_ptr(),
                      self.work.data_ptr(), self.work.numel() * self.work.element_size(), self.table.stride(0),
                      self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1], self.refused.data_ptr())

@@ -3,7 +3,9 @@ import ctypes as C
 import subprocess
 
 import pytest
+import torch
 
+import paper_2510_10129_amd as cc
 from paper_2510_10129_amd import build
 from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _Pool
 
@@ -38,3 +40,26 @@ def test_a_grow_that_is_not_waited_for_says_what_it_refused(lib):
     assert lib.grow(C.byref(_pool()), status) == lib.grow(C.byref(_pool(refused=A)), status) == CC_OK
     assert lib.grow(C.byref(_pool(refused=A)), None) == CC_OK and lib.grow(C.byref(_pool()), None) == CC_ERR_NULL
     assert lib.pool(C.byref(_pool(refused=A))) == CC_OK and lib.pool(C.byref(_pool(refused=A + 2))) == CC_ERR_SHAPE
+
+
+def test_assigned_fields_of_a_pool_are_checked():
+    """A pool whose tables were replaced is looked at again before the library is told of it."""
+    i32 = dict(dtype=torch.int32)
+
+    def assigned(**fields):
+        p = cc.PagePool.empty(8, 16, 3, 4, device="cpu")
+        p.c_struct()
+        for name, t in fields.items():
+            setattr(p, name, t)
+        return p.c_struct()
+
+    for bad in (dict(refs=torch.zeros(8, dtype=torch.int64)), dict(refs=torch.zeros(16, **i32)[::2]), dict(refs=torch.zeros(2, 4, **i32)),
+                dict(table=torch.zeros(3, 4, dtype=torch.int64)), dict(table=torch.zeros(2, 4, **i32)), dict(table=torch.zeros(4, 3, **i32).t()),
+                dict(table=torch.zeros(12, **i32)), dict(len=torch.zeros(3, dtype=torch.float64)), dict(len=torch.zeros(99, **i32)),
+                dict(table=torch.zeros(2, 4, dtype=torch.int64), len=torch.zeros(99, dtype=torch.float64)),
+                dict(table=torch.zeros(5, 4, **i32), len=torch.zeros(5, **i32)), dict(status=torch.zeros(1)), dict(status=torch.zeros(0, **i32)),
+                dict(work=torch.zeros(64, 64, dtype=torch.uint8).t()), dict(refused=torch.zeros(3)), dict(refused=torch.zeros(2, **i32))):
+        with pytest.raises(ValueError):
+            assigned(**bad)
+    longer = assigned(table=torch.zeros(5, 6, **i32), len=torch.zeros(5, **i32), refused=torch.zeros(5, **i32))
+    assert (longer.n_seqs, longer.max_pages, longer.stride_table) == (5, 6, 6)
