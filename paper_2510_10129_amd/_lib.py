@@ -366,6 +366,7 @@ class LayerWeights:
 
 class Context:
     """Owns a cc_ctx.  Methods mirror the C entry points one to one."""
+    _device = None                          # index of the GPU that it was created on
 
     def __init__(self, d, H_q, H_kv, d_h, f, rope_base, rms_eps, N_cap, M_cap, T_cap, stream=None):
         import torch
@@ -376,6 +377,7 @@ class Context:
         st = self._lib.cc_create(C.byref(self._h), C.byref(self.desc), C.c_void_p(s))
         if st != CC_OK:
             raise CacheClipError(st, (self._lib.cc_last_error(None) or b"").decode())
+        self._device = torch.cuda.current_device()
 
     @classmethod
     def for_model(cls, model, N_cap, M_cap, T_cap, stream=None):
@@ -521,8 +523,14 @@ class Context:
         n = len(kvs)
         return (_PagedKV * n).from_buffer(PagedKV.table(kvs, pool, self.desc)) if n else None, n
 
+    def _pool(self, pool: PagePool) -> _Pool:
+        """A pool's tensors lie together, and what comes with them lies there too (_on): on the host, perhaps."""
+        if pool.refs.get_device() != self._device:
+            raise ValueError("the pool must lie on the context's GPU")
+        return pool.c_struct()
+
     def _pages(self, call, pool: PagePool, sync: bool, *args):
-        p, host = pool.c_struct(), C.c_int32(0)
+        p, host = self._pool(pool), C.c_int32(0)
         self._check(call(self._h, C.byref(p), *args, C.byref(host) if sync else None))
 
     @staticmethod
@@ -569,7 +577,7 @@ class Context:
                 raise ValueError("pos must have an entry for each row")
             _on(pool, pos)
         _on(pool, q, k, v, q_out, new.start) if new.seq is None else _on(pool, q, k, v, q_out, new.start, new.seq)
-        p, kvs, r, rule = pool.c_struct(), kv.checked(pool, m), new.c_struct(), rope.c_struct()
+        p, kvs, r, rule = self._pool(pool), kv.checked(pool, m), new.c_struct(), rope.c_struct()
         self._check(self._lib.cc_step_rope_append(self._h, q.data_ptr(), st_q, k.data_ptr(), st_k, v.data_ptr(), st_v, C.byref(r),
                                                   _ptr(pos), C.byref(p), C.byref(kvs), C.byref(rule), q_out.data_ptr(), flags))
 
@@ -580,7 +588,7 @@ class Context:
             if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
                 raise ValueError(f"{what} must be contiguous")
         _on(pool, q, o, new.start, *(() if new.seq is None else (new.seq,)))
-        p, kvs, r = pool.c_struct(), kv.checked(pool, m), new.c_struct()
+        p, kvs, r = self._pool(pool), kv.checked(pool, m), new.c_struct()
         self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,
                                                       o.data_ptr(), flags))
 

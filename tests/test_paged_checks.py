@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2510_10129_amd as cc
-from paper_2510_10129_amd import build
+from paper_2510_10129_amd import _lib, build
 from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _Pool
 
 from test_paged_plan import A, CXX, _pool
@@ -63,3 +63,47 @@ def test_assigned_fields_of_a_pool_are_checked():
             assigned(**bad)
     longer = assigned(table=torch.zeros(5, 6, **i32), len=torch.zeros(5, **i32), refused=torch.zeros(5, **i32))
     assert (longer.n_seqs, longer.max_pages, longer.stride_table) == (5, 6, 6)
+
+
+class _NoCalls:
+    def __getattr__(self, name):
+        return lambda *args: pytest.fail("the library was called")
+
+
+def _calls(ctx, device):
+    """Every paged call, with all that it takes on one device."""
+    i32, bf = dict(dtype=torch.int32, device=device), dict(dtype=torch.bfloat16, device=device)
+    P, one = cc.PagePool.empty(8, 16, 3, 4, device=device), torch.zeros(1, **i32)
+    K, q, k = torch.zeros(8, 16, 2, 64, **bf), torch.zeros(1, 256, **bf), torch.zeros(1, 128, **bf)
+    kv, new = cc.PagedKV(K, K.clone()), cc.NewRows(torch.zeros(2, **i32), None, 1, 1)
+    return (lambda: ctx.grow_pages(P, [kv], one, one), lambda: ctx.fork_pages(P, one, one), lambda: ctx.free_pages(P, one),
+            lambda: ctx.compact_pages(P, [kv]), lambda: ctx.step_paged_attention(q, new, P, kv, q.clone()),
+            lambda: ctx.step_rope_append(q, k, k, new, P, kv, cc.Rope(1e4, 64), q))
+
+
+def test_a_pool_on_the_host_is_refused():
+    """All of it lies on one device, only not on a GPU."""
+    ctx = _lib.Context.__new__(_lib.Context)
+    ctx._lib, ctx._h = _NoCalls(), None
+    ctx.desc = _lib.ModelDesc(64, 4, 2, 64, 64, 1e4, 1e-5, 64, 64, 64)
+    for ctx._device in (None, 0, 1):
+        for call in _calls(ctx, "cpu"):
+            with pytest.raises(ValueError, match="context's GPU"):
+                call()
+
+
+@pytest.mark.gpu
+def test_a_pool_of_another_gpu_is_refused():
+    ctx = cc.Context(64, 4, 2, 64, 64, 1e4, 1e-5, N_cap=64, M_cap=64, T_cap=64)
+    assert ctx._device == torch.cuda.current_device()
+    ctx._device += 1                                        # as if it had been made there
+    for call in _calls(ctx, "cuda"):
+        with pytest.raises(ValueError, match="context's GPU"):
+            call()
+    ctx._device -= 1
+    P = cc.PagePool.empty(8, 16, 3, 4)
+    ctx.free_pages(P, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    P.len = P.len.cpu()
+    with pytest.raises(ValueError, match="pool's device"):
+        ctx.free_pages(P, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    ctx.close()
