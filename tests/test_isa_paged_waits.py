@@ -24,20 +24,43 @@ def kernels(tmp_path_factory):
 
 
 def tile_loop(body):
-    """The lines of the shortest cycle that the first LDS read written by hand lies in and a matrix instruction too: from the label that a
-    branch goes back to, to that branch, and the blocks behind it that end with a branch back into it."""
-    lines = body.split("\n")
-    at = {m.group(1): n for n, l in enumerate(lines) for m in [re.match(r"(\.LBB\d+_\d+):", l)] if m}
-    back = [(at[m.group(1)], n) for n, l in enumerate(lines) for m in [re.match(r"\ts_c?branch\S* (\.LBB\d+_\d+)", l)]
-            if m and m.group(1) in at and at[m.group(1)] <= n]
-    read = next(n for n, l in enumerate(lines) if l.startswith("\tds_read_b128") and "#ASMSTART" in lines[n - 1])
-    lo, hi = min(((t, b) for t, b in back if t <= read <= b and any("v_mfma" in l for l in lines[t:b])), key=lambda x: x[1] - x[0])
-    keep = list(range(lo, hi + 1))
-    for t, b in back:
-        if lo <= t <= hi < b:
-            block = max(n for n in at.values() if n <= b)
-            keep += [n for n in range(block, b + 1) if n not in keep]
-    return "\n".join(lines[n] for n in keep)
+    """The text of the basic blocks that can be reached from the first LDS read written by hand and reach it again without a barrier:
+    between two blocks of columns there is one, so what is left is the loop over tiles."""
+    blocks, at = [[]], {}
+    for n, line in enumerate(body.split("\n")):
+        label = re.match(r"(\.LBB\d+_\d+):", line)
+        if label:
+            blocks.append([])
+            at[label.group(1)] = len(blocks) - 1
+        blocks[-1].append(line)
+        if re.match(r"\ts_(?:c?branch|endpgm|setpc)", line):
+            blocks.append([])
+    after, before = {}, {}
+    for n, lines in enumerate(blocks):
+        to, last = set(), next((l for l in reversed(lines) if l.startswith("\ts_")), "")
+        if last.startswith("\ts_cbranch") or last.startswith("\ts_branch"):
+            to.add(at[last.split()[1]])
+        if not re.match(r"\ts_(?:branch|endpgm|setpc)", last) and n + 1 < len(blocks):
+            to.add(n + 1)
+        if any(l.startswith("\ts_barrier") for l in lines):
+            to = set()
+        after[n] = to
+        for t in to:
+            before.setdefault(t, set()).add(n)
+
+    def reach(n, edges):
+        seen, todo = set(), [n]
+        while todo:
+            for t in edges.get(todo.pop(), ()):
+                if t not in seen:
+                    seen.add(t)
+                    todo.append(t)
+        return seen
+
+    read = next(n for n, lines in enumerate(blocks) if re.search(r"#ASMSTART\n\tds_read_b128", "\n".join(lines)))
+    loop = reach(read, after) & reach(read, before)
+    assert read in loop
+    return "\n".join("\n".join(blocks[n]) for n in sorted(loop))
 
 
 def load_waits(text):
