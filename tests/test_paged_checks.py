@@ -7,7 +7,7 @@ import torch
 
 import paper_2510_10129_amd as cc
 from paper_2510_10129_amd import _lib, build
-from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _Pool
+from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _NewRows, _Pool
 
 from test_paged_plan import A, CXX, _pool
 
@@ -17,6 +17,7 @@ extern "C" {
 int pool(const cc_page_pool* p) { return cc_check_pool(p).code; }
 int grow(const cc_page_pool* p, const int32_t* status) { return cc_check_grow(*p, status).code; }
 int pool_size() { return sizeof(cc_page_pool); }
+int attend(const cc_new_rows* r, const cc_page_pool* p, int g, int window, int sinks) { return cc_check_attend(*r, *p, g, window, sinks).code; }
 }
 """
 
@@ -40,6 +41,37 @@ def test_a_grow_that_is_not_waited_for_says_what_it_refused(lib):
     assert lib.grow(C.byref(_pool()), status) == lib.grow(C.byref(_pool(refused=A)), status) == CC_OK
     assert lib.grow(C.byref(_pool(refused=A)), None) == CC_OK and lib.grow(C.byref(_pool()), None) == CC_ERR_NULL
     assert lib.pool(C.byref(_pool(refused=A))) == CC_OK and lib.pool(C.byref(_pool(refused=A + 2))) == CC_ERR_SHAPE
+
+
+def _attend(lib, rows, n, max_pages, page=64, g=1, window=0, sinks=0):
+    return lib.attend(C.byref(_NewRows(A, A, n, rows, 1)), C.byref(_pool(max_pages=max_pages, page_size=page, stride_table=1 << 26)), g, window, sinks)
+
+
+def test_attention_checks(lib):
+    assert _attend(lib, 10, 3, 8) == _attend(lib, 10, 3, 8, window=2 ** 31 - 1, sinks=2 ** 31 - 1) == _attend(lib, 0, 0, 8) == CC_OK
+    assert _attend(lib, 10, 3, 8, window=-1) == _attend(lib, 10, 3, 8, sinks=-1) == CC_ERR_SHAPE
+    # blocks times tiles below 2^31: 128 sequences of a row, 2^24 tiles of 64 keys with the 8 that a block costs besides its own
+    for rows, n, g in ((128, 128, 1), (127 * 256, 1, 1), (127 * 32, 1, 8), (64 * 32, 64, 8)):
+        assert _attend(lib, rows, n, (1 << 24) - 9, g=g) == CC_OK
+        assert _attend(lib, rows, n, (1 << 24) - 8, g=g) == CC_ERR_SHAPE
+    # 64 keys a tile, whatever the page
+    assert _attend(lib, 128, 128, 4 * ((1 << 24) - 9), page=16) == CC_OK and _attend(lib, 128, 128, 4 * ((1 << 24) - 9) + 1, page=16) == CC_ERR_SHAPE
+
+
+def test_units_of_the_largest_attention_call_fit_32_bits(lib):
+    """The many-rows kernel counts key tiles in 32 bits: its blocks' tiles, 5 more a block, rounded up to whole ranges where no more
+    blocks than workgroups are there (ranges of the longest block over the workgroups that a block can have, 8 at least)."""
+    for n in list(range(1, 300)) + [511, 512, 1000, 1024]:
+        tiles = min((1 << 24) - 1, (2 ** 31 - 1) // n - 8)
+        assert _attend(lib, 0, n, tiles) == CC_OK and (tiles == (1 << 24) - 1 or _attend(lib, 0, n, tiles + 1) == CC_ERR_SHAPE)
+        length = tiles + 5
+        for workgroups in (64, 128, 256):
+            for heads in (1, 2, 4, 8):
+                units = n * length
+                if n * heads <= workgroups:
+                    each = max(8, -(-length // (workgroups // (n * heads))))
+                    units = n * (-(-length // each) * each)
+                assert units < 2 ** 31, (n, workgroups, heads)
 
 
 def test_assigned_fields_of_a_pool_are_checked():
