@@ -371,8 +371,8 @@ typedef struct cc_rope {
  * q, k or v).
  * pos dev int32 [rows], or NULL: the position each row turns by where it is not the row's place in the sequence.
  * A sequence must not be listed twice, and a page that another sequence also holds is written all the same:
- * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths, the written pages and that no grow of
- * a sequence with rows was refused first; without it, rows in front of their sequence's first token and rows of a sequence whose grow
+ * cc_grow_pages makes the copies.  flags: CC_FLAG_CHECK_IDX verifies start, seq, the lengths, the written pages and that no sequence
+ * has rows twice or a refused grow first; without it, rows in front of their sequence's first token and rows of a sequence whose grow
  * was refused are skipped: no key, value or query of theirs is written. */
 cc_status cc_step_rope_append(cc_ctx* ctx, const void* q, int64_t stride_q, const void* k, int64_t stride_k,
                               const void* v, int64_t stride_v, const cc_new_rows* rows, const int32_t* pos,

@@ -125,7 +125,7 @@ cc_status check_rows_sync(cc_ctx* c, const cc_new_rows& r, const cc_page_pool& p
     CC_HIP(c, hipMemcpyAsync(c->pinned, c->flag, sizeof(int32_t), hipMemcpyDeviceToHost, c->stream));
     CC_HIP(c, hipStreamSynchronize(c->stream));
     if (c->pinned[0] != 0)
-        return fail(c, CC_ERR_IDX, "start must ascend within rows, seq be in range, a sequence be as long as its new rows, its pages be in range and its last grow not be refused");
+        return fail(c, CC_ERR_IDX, "start must ascend within rows, seq be in range (and written once), a sequence be as long as its new rows, its pages be in range and its last grow not be refused");
     return CC_OK;
 }
 

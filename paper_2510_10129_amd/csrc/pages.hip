@@ -408,6 +408,9 @@ __global__ __launch_bounds__(64) void check_rows_kernel(const int32_t* __restric
         const int n = r1 - r0, L = p.len[s];
         bad = L < n || L > (int64_t)p.max_pages << p.shift || (append && n > 0 && p.refused && p.refused[s] != 0);
         if (!bad && n > 0) {
+            // a sequence's last places belong to one set of rows
+            if (append && seq)
+                for (int i = lane; i < b; i += 64) bad |= seq[i] == s && start[i + 1] > start[i];
             const int first = L - n;
             const int low = append ? first : window > 0 ? max(0, first - window + 1) : 0;
             const int seen = append ? 0 : min(low, sinks);

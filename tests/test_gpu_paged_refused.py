@@ -147,3 +147,25 @@ def test_a_captured_loop_that_runs_out_of_pages():
     for s in range(3):
         assert np.array_equal(host_bits(kv.V[pool.table[s, kept[s] // PAGE].item(), kept[s] % PAGE]), host_bits(parts[2][s]).reshape(H_KV, D_H))
     ctx.close()
+
+
+def test_a_sequence_with_two_sets_of_rows_is_reported():
+    """Its last places would be written by both: the index check of the append refuses it; a second entry without rows is none."""
+    rng = np.random.default_rng(63)
+    pool, kv = _make(rng, 80, 70)
+    ctx = _ctx(H_Q, H_KV, D_H)
+    ctx.grow_pages(pool, [kv], dev_i32(range(70)), dev_i32([9] * 70))
+    before = _bits(pool, kv)
+    for seqs, more, ok in (([4, 5, 4], [1, 1, 1], False), ([4, 5, 4], [1, 1, 0], True), ([4, 5, 4], [0, 1, 2], True),
+                           (list(range(70)) + [0], [1] * 71, False), (list(range(69)) + [68], [1] * 70, False), (list(range(70)), [1] * 70, True)):
+        new, parts = _rows(rng, seqs, more)
+        out = torch.full((new.rows, H_Q * D_H), 7.0, dtype=torch.bfloat16, device=DEV)
+        if ok:
+            ctx.step_rope_append(*parts, new, pool, kv, RULE, out, flags=_lib.FLAG_CHECK_IDX)
+            before = _bits(pool, kv)
+            continue
+        with pytest.raises(cc.CacheClipError) as e:
+            ctx.step_rope_append(*parts, new, pool, kv, RULE, out, flags=_lib.FLAG_CHECK_IDX)
+        assert e.value.status == _lib.CC_ERR_IDX and _same(_bits(pool, kv), before) and bool((out == 7.0).all())
+        ctx.step_paged_attention(out, new, pool, kv, torch.empty_like(out), flags=_lib.FLAG_CHECK_IDX)      # may look twice
+    ctx.close()
