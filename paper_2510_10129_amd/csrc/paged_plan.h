@@ -143,7 +143,7 @@ inline cc_refusal cc_check_rope(const cc_rope* r, int32_t d_h) {
     CC_REFUSE_IF(!(r->base > 1.0) || !std::isfinite(r->base), CC_ERR_SHAPE, "base must be finite and > 1");
     CC_REFUSE_IF(r->rot < 2 || r->rot > d_h || r->rot % 2, CC_ERR_SHAPE, "rot must be even and in [2, d_h]");
     CC_REFUSE_IF(r->scaling < CC_ROPE_PLAIN || r->scaling > CC_ROPE_INDEX, CC_ERR_SHAPE, "unknown scaling");
-    CC_REFUSE_IF(!std::isfinite(r->mscale), CC_ERR_SHAPE, "mscale must be finite");
+    CC_REFUSE_IF(!(std::fabs(r->mscale) <= 3.4e38), CC_ERR_SHAPE, "mscale must be finite in 32 bits");
     CC_REFUSE_IF(r->scaling != CC_ROPE_PLAIN && (!(r->factor >= 1.0) || !std::isfinite(r->factor)), CC_ERR_SHAPE,
                  "factor must be finite and >= 1");
     CC_REFUSE_IF(r->scaling >= CC_ROPE_TURNS && (r->orig_len < 1 || !(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high)),

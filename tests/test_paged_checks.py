@@ -7,7 +7,7 @@ import torch
 
 import paper_2510_10129_amd as cc
 from paper_2510_10129_amd import _lib, build
-from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _NewRows, _Pool
+from paper_2510_10129_amd._lib import CC_ERR_NULL, CC_ERR_SHAPE, CC_OK, _NewRows, _Pool, _Rope
 
 from test_paged_plan import A, CXX, _pool
 
@@ -16,6 +16,7 @@ SHIM = r"""
 extern "C" {
 int pool(const cc_page_pool* p) { return cc_check_pool(p).code; }
 int grow(const cc_page_pool* p, const int32_t* status) { return cc_check_grow(*p, status).code; }
+int rope(const cc_rope* r, int d_h) { return cc_check_rope(r, d_h).code; }
 int pool_size() { return sizeof(cc_page_pool); }
 int attend(const cc_new_rows* r, const cc_page_pool* p, int g, int window, int sinks) { return cc_check_attend(*r, *p, g, window, sinks).code; }
 }
@@ -41,6 +42,12 @@ def test_a_grow_that_is_not_waited_for_says_what_it_refused(lib):
     assert lib.grow(C.byref(_pool()), status) == lib.grow(C.byref(_pool(refused=A)), status) == CC_OK
     assert lib.grow(C.byref(_pool(refused=A)), None) == CC_OK and lib.grow(C.byref(_pool()), None) == CC_ERR_NULL
     assert lib.pool(C.byref(_pool(refused=A))) == CC_OK and lib.pool(C.byref(_pool(refused=A + 2))) == CC_ERR_SHAPE
+
+
+def test_a_scale_that_32_bits_cannot_hold(lib):
+    for mscale, code in ((3e38, CC_OK), (-3e38, CC_OK), (1e39, CC_ERR_SHAPE), (-1e300, CC_ERR_SHAPE), (float("inf"), CC_ERR_SHAPE),
+                         (float("nan"), CC_ERR_SHAPE)):
+        assert lib.rope(C.byref(_Rope(base=1e4, rot=2, mscale=mscale)), 64) == code, mscale
 
 
 def _attend(lib, rows, n, max_pages, page=64, g=1, window=0, sinks=0):
