@@ -191,6 +191,13 @@ def _i32(t, what: str, dims: int = 1):
     return t
 
 
+def _int32(v: int, what: str) -> int:
+    """A number as the library takes it: what does not fit would lose its upper half on the way."""
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError(f"{what} must be a 32-bit integer")
+    return v
+
+
 def _bf16(t, what: str):
     if t.dtype is not _torch.bfloat16:
         raise ValueError(f"{what} must be a bfloat16 tensor")
@@ -280,7 +287,9 @@ class PagePool(_Described):
         self._check()
         return _Pool(self.refs.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.status.data_ptr(),
                      self.work.data_ptr(), self.work.numel() * self.work.element_size(), self.table.stride(0),
-                     self.refs.numel(), self.page_size, self.len.numel(), self.table.shape[1], self.refused.data_ptr())
+                     _int32(self.refs.numel(), "the number of pages"), _int32(self.page_size, "page_size"),
+                     _int32(self.len.numel(), "the number of sequences"), _int32(self.table.shape[1], "the table's width"),
+                     self.refused.data_ptr())
 
 
 @dataclass
@@ -325,7 +334,8 @@ class NewRows(_Described):
         n = _i32(self.start, "start").numel() - 1
         if n < 0 or (self.seq is not None and _i32(self.seq, "seq").numel() != n):
             raise ValueError("start must have one entry more than seq")
-        return _NewRows(self.start.data_ptr(), _ptr(self.seq), n, self.rows, self.max_new)
+        return _NewRows(self.start.data_ptr(), _ptr(self.seq), _int32(n, "the number of sequences"), _int32(self.rows, "rows"),
+                        _int32(self.max_new, "max_new"))
 
 
 @dataclass
@@ -344,8 +354,8 @@ class Rope(_Described):
     def _describe(self) -> _Rope:
         if self.scaling not in ROPE_SCALINGS:
             raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
-        return _Rope(self.base, self.rot, int(self.interleaved), ROPE_SCALINGS.index(self.scaling), self.orig_len, self.factor,
-                     self.low, self.high, self.mscale)
+        return _Rope(self.base, _int32(self.rot, "rot"), int(bool(self.interleaved)), ROPE_SCALINGS.index(self.scaling),
+                     _int32(self.orig_len, "orig_len"), self.factor, self.low, self.high, self.mscale)
 
 
 @dataclass
@@ -587,6 +597,7 @@ class Context:
         for t, what in ((q, "q"), (o, "o")):
             if self._row_buffer(t, what, new.rows, m.H_q * m.d_h) != m.H_q * m.d_h:
                 raise ValueError(f"{what} must be contiguous")
+        _int32(window, "window"), _int32(sinks, "sinks")
         _on(pool, q, o, new.start, *(() if new.seq is None else (new.seq,)))
         p, kvs, r = self._pool(pool), kv.checked(pool, m), new.c_struct()
         self._check(self._lib.cc_step_paged_attention(self._h, q.data_ptr(), C.byref(r), C.byref(p), C.byref(kvs), window, sinks,

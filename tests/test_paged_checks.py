@@ -146,3 +146,24 @@ def test_a_pool_of_another_gpu_is_refused():
     with pytest.raises(ValueError, match="pool's device"):
         ctx.free_pages(P, torch.zeros(1, dtype=torch.int32, device="cuda"))
     ctx.close()
+
+
+def test_numbers_that_do_not_fit_32_bits_are_refused():
+    """A window of 2^32 + 5 is not one of 5."""
+    big, start = (1 << 32) + 16, torch.zeros(3, dtype=torch.int32)
+    for make in (lambda: cc.NewRows(start, None, big, 2), lambda: cc.NewRows(start, None, 4, big), lambda: cc.Rope(1e4, big),
+                 lambda: cc.Rope(1e4, 64, scaling="turns", orig_len=1 << 31)):
+        with pytest.raises(ValueError, match="32-bit"):
+            make().c_struct()
+    P = cc.PagePool.empty(8, 16, 3, 4, device="cpu")
+    P.page_size = big
+    with pytest.raises(ValueError, match="32-bit"):
+        P.c_struct()
+    assert cc.Rope(1e4, 64, interleaved=1 << 32).c_struct().interleaved == 1
+    ctx = _lib.Context.__new__(_lib.Context)
+    ctx._lib, ctx._h, ctx._device = _NoCalls(), None, -1
+    ctx.desc = _lib.ModelDesc(64, 4, 2, 64, 64, 1e4, 1e-5, 64, 64, 64)
+    P, K, q = cc.PagePool.empty(8, 16, 3, 4, device="cpu"), torch.zeros(8, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(5, 256, dtype=torch.bfloat16)
+    for kw in (dict(window=big), dict(window=5, sinks=1 << 31)):
+        with pytest.raises(ValueError, match="32-bit"):
+            ctx.step_paged_attention(q, cc.NewRows(start, None, 5, 5), P, cc.PagedKV(K, K), q.clone(), **kw)
