@@ -264,6 +264,8 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
  * question), answers that fork from one context, and what is freed behind them.  Keys and values live in pages of
  * page_size tokens that sequences hold by reference.  A cache of cc_recompute_layer becomes pages without a copy
  * when its slots are a multiple of page_size: stride_page = page_size * stride_token, page i = slots i*page_size ...
+ * (its keys are turned by the context's rule: rot = d_h, halves, rope_base).  Queries, keys and values of new rows are the caller's own
+ * products; none of a call's other buffers may lie in the pages.
  *
  * All of it is device memory of the caller, and every change is made on the device in stream order, so that a decode
  * loop needs no host round trip and can be captured.
@@ -278,7 +280,8 @@ cc_status cc_assemble_cache(cc_ctx* ctx, const cc_chunk_kv* chunks, int32_t n_ch
  *           (so may the caller).  While it is not 0, cc_step_rope_append skips the sequence's rows: their places do not exist, and
  *           the last ones of the unchanged length hold other tokens.  NULL is for programs that wait for every grow's status.
  *   work    cc_page_work_bytes(n_pages, n_seqs) bytes, 256-byte aligned: scratch, its contents mean nothing
- *           between calls.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
+ *           between calls.  69 MB of it, whatever the pool, are for what attention leaves of blocks that it cuts; the rest is up to
+ *           32 bytes a page and a sequence.  Calls that use one pool must not overlap (two streams, two captured graphs replayed
  *           at once), whatever context they come from; nor must two attention calls of one context, whatever
  *           their pools.
  * page_size is a power of two, 16 to 1024; n_seqs <= 65536, n_pages * page_size < 2^31, max_pages * page_size < 2^30. */
