@@ -37,8 +37,8 @@ inline cc_page_work cc_page_work_layout(int64_t n_pages, int64_t n_seqs) {
 
 // Which attention kernel takes a batch whose sequences have up to so many (row, query head of a group) columns: few rows read
 // every key once per 16 columns (32 at d_h = 64) from a ring a wave, many rows multiply 256 columns a workgroup.  16 sequences of 4000
-// to 12000 tokens, us few / many:  d_h = 128, 32 heads of 8, 4 columns 100 / 111, 16 columns 95 / 101, 20 columns (two blocks of 16 a
-// wave) 147 / 106;  d_h = 64, 32 of 8, 4 columns 61 / 79, 32 columns 66 / 79, 64 columns (four blocks) 114 / 88.  So a single token
+// to 12000 tokens, us few / many:  d_h = 128, 32 heads of 8, 4 columns 97 / 98, 16 columns 98 / 98, 20 columns (two blocks of 16 a
+// wave) 147 / 106;  d_h = 64, 32 of 8, 4 columns 58 / 72, 32 columns 59 / 72, 64 columns (four blocks) 114 / 88.  So a single token
 // of more than 16 query heads a kv head is a call of many rows at d_h = 128: 32 ragged sequences of up to 16577 tokens, 32 heads of 1
 // 46 us (176 MB) and 64 of 2 73 (351 MB), where 16 of 1 and 32 of 2 take 37 and 66.
 inline bool cc_few_rows(int64_t columns, int32_t d_h) { return columns <= (d_h == 128 ? 16 : 32); }
