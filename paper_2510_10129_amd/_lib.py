@@ -264,6 +264,9 @@ class PagePool(_Described):
             self.work = torch.empty(size, dtype=torch.uint8, device=self.refs.device)
         if self.refused is None:
             self.refused = torch.zeros_like(self.len)
+            # a context's stream need not wait for torch's, and what the memory held before would read as refusals
+            if self.len.is_cuda and not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream(self.len.device).synchronize()
         self._check()
 
     def _check(self):

@@ -169,3 +169,31 @@ def test_a_sequence_with_two_sets_of_rows_is_reported():
         assert e.value.status == _lib.CC_ERR_IDX and _same(_bits(pool, kv), before) and bool((out == 7.0).all())
         ctx.step_paged_attention(out, new, pool, kv, torch.empty_like(out), flags=_lib.FLAG_CHECK_IDX)      # may look twice
     ctx.close()
+
+
+def test_a_new_pool_is_ready_for_every_stream():
+    """The words of a new pool lie in memory that held other numbers, and torch's stream is busy: a context on a stream of its own does
+    not wait for it."""
+    rng = np.random.default_rng(64)
+    made, kv = _make(rng, 8, 3)
+    side = torch.cuda.Stream()
+    ctx = _ctx(H_Q, H_KV, D_H, stream=side.cuda_stream)
+    new, parts = _rows(rng, [0, 1, 2], [4, 1, 20])
+    q = torch.zeros((25, H_Q * D_H), dtype=torch.bfloat16, device=DEV)
+    torch.cuda.synchronize()
+    ctx.grow_pages(made, [kv], dev_i32([0, 1, 2]), dev_i32([4, 1, 20]))
+    x = torch.randn((4096, 4096), device=DEV)
+    old = [torch.full((3,), -4, dtype=torch.int32, device=DEV) for _ in range(200)]
+    torch.cuda.synchronize()
+    del old
+    for _ in range(20):
+        y = x @ x                                           # some milliseconds
+    pool = cc.PagePool(made.refs, made.table, made.len, PAGE, status=made.status, work=made.work)
+    ctx.step_rope_append(*parts, new, pool, kv, RULE, q)
+    torch.cuda.synchronize()
+    del y
+    assert pool.status.item() == 0 and not pool.refused.any() and bool(q.any(dim=1).all())
+    for s, (r0, n) in enumerate(((0, 4), (4, 1), (5, 20))):
+        pages, pos = pool.table[s].cpu().numpy(), np.arange(n)
+        assert np.array_equal(host_bits(kv.V)[pages[pos // PAGE], pos % PAGE], host_bits(parts[2][r0:r0 + n]).reshape(n, H_KV, D_H))
+    ctx.close()
